@@ -398,6 +398,69 @@ int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
                         int64_t n, int32_t n_classes, void* dlogits, int64_t ldd, double* loss,
                         void* stream);
 
+/*
+ * The same loss of a linear last layer, whose logits are never stored: with S = H W over the N rows that have a
+ * label (0 <= label < n_classes; any other value: a row without one),
+ *   row_loss[r] = log sum_c exp S[r, c] - S[r, label],   loss = mean of it over the N rows,
+ *   dH = P W^T,  dW = H^T P,  P = (softmax(S) - onehot) / N.
+ * Rows without a label cost nothing, whatever they hold; their rows of dH and row_loss become zero.  Without any
+ * labelled row, loss, dH and dW are zero.
+ *   H, dH   : n x k, `dtype`.  dH may be H itself (same pointer and pitch).     W, dW : k x n_classes, fp32.
+ *   labels  : [n].     row_loss : [n] fp32.     loss : one device double.
+ *   loss, row_loss, dH and dW may each be NULL (at least one is wanted); without dH and dW the call is the forward
+ *   pass alone, and one row is scored like any number of them.
+ * The classes are walked in pieces: largest logit and sum of exponentials of a row first, then, for the gradients,
+ * the logits again.  Products run on the f16 matrix cores with fp32 sums, an fp32 operand as two f16 terms (22 bits
+ * and more), a bf16 one as one; columns of H and rows of W are scaled by powers of two, so that an element keeps its
+ * bits down to 2^-17 of the largest magnitude in its column of H (row of W), and below is off by 2^-39 of that at
+ * most.  (Features whose largest H and W multiply to 2^-d of the most of all features have 2^(d/2) less of this
+ * room.)  A probability is resolved to 2^-40.  dH of bf16 features is a product of one term each: off by 2^-11 of
+ * its terms, an eighth of the rounding to bf16 that follows.  A row whose logits are not all finite numbers has a
+ * loss and gradients that are NaN.
+ *   workspace : device memory of mixgcn_linear_xent_workspace(...) bytes, 256-byte aligned, which the call uses
+ *   until its work on the stream is done (calls that overlap need one each).  The call allocates nothing and does
+ *   not synchronise.  mixgcn_linear_xent_workspace (host arithmetic; gradients: whether dH or dW is wanted) is -1
+ *   for bad sizes: at most 2^30 rows, 2^16 features, 2^24 classes.
+ */
+int64_t mixgcn_linear_xent_workspace(int dtype, int64_t n, int32_t k, int32_t n_classes, int gradients);
+int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, int64_t ldw, const int32_t* labels,
+                       int64_t n, int32_t k, int32_t n_classes, double* loss, float* row_loss, void* dH, int64_t ldd,
+                       float* dW, int64_t ldg, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Activations kept in 8 bits for the backward pass.  32 consecutive columns of a row share a power of two 2^s; an
+ * element is code * 2^s.
+ *   codes     : [n_rows] x ld_codes signed bytes (16-byte aligned, ld_codes a multiple of 16), -127 .. 127.
+ *   exponents : [n_rows] x ld_exponents bytes, s + 133 of columns 32 g .. 32 g + 31 at place g
+ *               (ld_exponents >= ceil(n_cols / 32)).
+ * mixgcn_checkpoint_pack takes the smallest s >= -133 at which the group's largest magnitude is rounded to 127 at most,
+ * and rounds x / 2^s to the nearest code, ties to even: an element is off by 2^s / 2, at most 1/127 of the group's
+ * largest, and the codes do not depend on anything but x.  What is not finite is left out of s and has the code
+ * -128, which is read back as NaN.  Codes of the row padding up to whole 16 bytes become zero.
+ * mixgcn_checkpoint_unpack writes code * 2^s, which is a bf16 number and so exact in either type; the row padding of X
+ * stays as it is.
+ */
+int mixgcn_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n_rows, int32_t n_cols, int8_t* codes,
+                           int64_t ld_codes, uint8_t* exponents, int64_t ld_exponents, void* stream);
+int mixgcn_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ld_codes, const uint8_t* exponents,
+                             int64_t ld_exponents, int64_t n_rows, int32_t n_cols, void* X, int64_t ldx, void* stream);
+
+/*
+ * The weight gradient of a layer whose input was kept in 8 bits: dW[k x m] = beta dW + Z^T (G (.) M), Z [n_rows x k]
+ * the checkpoint, G [n_rows x m] of `dtype`, M an optional bitmap (the form of mixgcn_relu_bitmap; NULL: none), dW
+ * fp32, beta 0 or 1.  The values of Z and bf16 gradients enter the bf16 matrix cores as they are, fp32 gradients
+ * as the exact sum of three bf16 terms; sums are fp32, and those of the row slabs are joined in 64 bits in a fixed
+ * order.  Infinities and NaN give what fp32 arithmetic gives.  What a masked element of G holds does not matter.
+ *   workspace : device memory of mixgcn_checkpoint_wgrad_workspace(n_rows, k, m) bytes (-1 for bad sizes), 16-byte
+ *   aligned, which the call uses until its work on the stream is done.  The call allocates nothing and does not
+ *   synchronise.
+ */
+int64_t mixgcn_checkpoint_wgrad_workspace(int64_t n_rows, int32_t k, int32_t m);
+int mixgcn_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ld_codes, const uint8_t* exponents,
+                            int64_t ld_exponents, const void* G, int64_t ldg, float* dW, int64_t ldw, int64_t n_rows,
+                            int32_t k, int32_t m, const uint32_t* mask, int64_t ld_mask, float beta, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
 /* Helpers. */
 int mixgcn_graph_info(const mixgcn_graph* g, mixgcn_graph_view* out);
 int mixgcn_graph_free(mixgcn_graph* g);

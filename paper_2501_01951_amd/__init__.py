@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     apply_bitmap,
     backward_pipelined, bandwidth, build_csr, dropout_bitmap, forward_pipelined, pipeline_window,
     cu_subset_stream,
+    Checkpoint, checkpoint_pack, checkpoint_unpack, checkpoint_wgrad, checkpoint_wgrad_workspace,
+    linear_xent, linear_xent_workspace,
     layer_bwd, layer_fwd, lib_path, load_library, measure_peaks, normalize, permute_rows, pipeline_stages, relabel_edges, release_memory,
     relu_bitmap, reorder_rcm, set_aggregate_whole_rows, set_update_arith, softmax_xent, update, version,
 )

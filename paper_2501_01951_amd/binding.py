@@ -107,6 +107,16 @@ def load_library():
                                            ctypes.POINTER(ctypes.c_int32),
                                            ctypes.POINTER(ctypes.c_int32)]
     lib.mixgcn_softmax_xent.argtypes = [ctypes.c_int, vp, i64, vp, i64, i32, vp, i64, vp, vp]
+    lib.mixgcn_linear_xent_workspace.argtypes = [ctypes.c_int, i64, i32, i32, ctypes.c_int]
+    lib.mixgcn_linear_xent_workspace.restype = i64
+    lib.mixgcn_linear_xent.argtypes = [ctypes.c_int, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, i64, vp, i64,
+                                       vp, i64, vp]
+    lib.mixgcn_checkpoint_pack.argtypes = [ctypes.c_int, vp, i64, i64, i32, vp, i64, vp, i64, vp]
+    lib.mixgcn_checkpoint_unpack.argtypes = [ctypes.c_int, vp, i64, vp, i64, i64, i32, vp, i64, vp]
+    lib.mixgcn_checkpoint_wgrad_workspace.argtypes = [i64, i32, i32]
+    lib.mixgcn_checkpoint_wgrad_workspace.restype = i64
+    lib.mixgcn_checkpoint_wgrad.argtypes = [ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, vp, i64,
+                                            f32, vp, i64, vp]
     lib.mixgcn_set_update_arith.argtypes = [ctypes.c_int]
     lib.mixgcn_set_update_arith.restype = ctypes.c_int
     lib.mixgcn_set_aggregate_whole_rows.argtypes = [ctypes.c_int]
@@ -124,7 +134,8 @@ def load_library():
     for name in ("release_memory", "build_csr", "normalize", "aggregate", "aggregate_masked", "relu_bitmap",
                  "measure_peaks", "reorder_rcm", "bandwidth", "relabel_edges", "permute_rows",
                  "update", "layer_fwd", "layer_bwd",
-                 "softmax_xent", "graph_info", "graph_free", "pipeline_create", "pipeline_destroy",
+                 "softmax_xent", "linear_xent", "checkpoint_pack", "checkpoint_unpack", "checkpoint_wgrad",
+                 "graph_info", "graph_free", "pipeline_create", "pipeline_destroy",
                  "pipeline_timing", "pipeline_timing_read", "stream_create_cu_subset", "stream_destroy"):
         getattr(lib, "mixgcn_" + name).restype = ctypes.c_int
     _lib = lib
@@ -526,3 +537,138 @@ def softmax_xent(logits, labels, dlogits, loss, stream=None) -> None:
                                               _ptr(labels), n, c,
                                               _ptr(dlogits), _ld(dlogits), _ptr(loss),
                                               _stream(stream)), "softmax_xent")
+
+
+class _on:
+    """The device of a call's tensors made current where it is not, and its stream, with which the call's
+    workspace is allocated (so that it is given back in that stream's order, and belongs to a graph that
+    is being captured there).  All tensors of a call are on one device."""
+
+    def __init__(self, stream, *tensors):
+        self.device = tensors[0].device
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"tensors on {self.device} and {t.device}")
+        if self.device.type != "cuda":
+            raise ValueError("tensors on a GPU expected")
+        # a stream belongs to its device: entering its context makes both current
+        self._ctx = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(self.device)
+
+    def __enter__(self):
+        self._ctx.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        return self._ctx.__exit__(*exc)
+
+    def workspace(self, given, need: int):
+        if given is None:
+            return torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
+        if given.device != self.device or not given.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor on the device of the others expected")
+        return given
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def _shape(what: str, t, *shape, dtype=None) -> None:
+    if t is not None and (tuple(t.shape) != shape or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, expected {shape}" + (f" {dtype}" if dtype else ""))
+
+
+def linear_xent_workspace(dtype, n: int, k: int, n_classes: int, gradients: bool = True) -> int:
+    """Bytes of workspace of linear_xent for n x k features of a torch dtype."""
+    code = {torch.float32: F32, torch.bfloat16: BF16}[dtype]
+    return load_library().mixgcn_linear_xent_workspace(code, n, k, n_classes, int(gradients))
+
+
+def linear_xent(H, W, labels, loss=None, dH=None, dW=None, row_loss=None, workspace=None, stream=None) -> None:
+    """Mean softmax cross-entropy of the linear layer H W and its gradients without the logits.  labels: int32
+    [n], a row whose label is not in [0, n_classes) has none and costs nothing.  Any of loss (float64 [1]),
+    row_loss (float32 [n]), dH (like H; may be H) and dW (like W) is computed that is given.  workspace: device
+    memory of linear_xent_workspace bytes to use instead of allocating it."""
+    n, k = H.shape
+    c = W.shape[1]
+    _shape("W", W, k, c, dtype=torch.float32)
+    _shape("labels", labels, n, dtype=torch.int32)
+    _shape("loss", loss, 1, dtype=torch.float64)
+    _shape("row_loss", row_loss, n, dtype=torch.float32)
+    _shape("dH", dH, n, k, dtype=H.dtype)
+    _shape("dW", dW, k, c, dtype=torch.float32)
+    for t in (labels, row_loss):
+        if t is not None and not t.is_contiguous():
+            raise ValueError("labels and row_loss: contiguous tensors expected")
+    with _on(stream, H, W, labels, loss, dH, dW, row_loss) as on:
+        ws = on.workspace(workspace, linear_xent_workspace(H.dtype, n, k, c, dH is not None or dW is not None))
+        _check(load_library().mixgcn_linear_xent(
+            _dtype_of(H), _ptr(H), _ld(H), _ptr(W), _ld(W), _ptr(labels), n, k, c, _ptr(loss), _ptr(row_loss), _ptr(dH),
+            _ld(dH) if dH is not None else 0, _ptr(dW), _ld(dW) if dW is not None else 0, _ptr(ws), _nbytes(ws),
+            _stream(stream)), "linear_xent")
+
+
+class Checkpoint:
+    """Activations kept in 8 bits: codes (int8 [n, cols], rows on a pitch of whole 16 bytes) and exponents (uint8
+    [n, ceil(cols / 32)]); the layout is the one of mixgcn_checkpoint_pack."""
+
+    def __init__(self, codes, exponents):
+        if codes.dim() != 2 or codes.dtype != torch.int8:
+            raise ValueError("codes: int8 [n, cols] expected")
+        n, cols = codes.shape
+        _shape("exponents", exponents, n, (cols + 31) // 32, dtype=torch.uint8)
+        self.codes, self.exponents = codes, exponents
+
+    @classmethod
+    def empty(cls, n: int, cols: int, device="cuda"):
+        codes = torch.empty(n, (cols + 15) // 16 * 16, dtype=torch.int8, device=device)[:, :cols]
+        return cls(codes, torch.empty(n, (cols + 31) // 32, dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+
+def checkpoint_pack(X, kept: Checkpoint = None, stream=None) -> Checkpoint:
+    """X to 8 bits."""
+    n, cols = X.shape
+    with _on(stream, X, *((kept.codes, kept.exponents) if kept is not None else ())):
+        if kept is None:
+            kept = Checkpoint.empty(n, cols, X.device)
+        _shape("codes", kept.codes, n, cols)
+        _check(load_library().mixgcn_checkpoint_pack(
+            _dtype_of(X), _ptr(X), _ld(X), n, cols, _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents),
+            _ld(kept.exponents), _stream(stream)), "checkpoint_pack")
+    return kept
+
+
+def checkpoint_unpack(kept: Checkpoint, X, stream=None) -> None:
+    """The values of a checkpoint into X (n x cols, float32 or bfloat16)."""
+    n, cols = kept.shape
+    _shape("X", X, n, cols)
+    with _on(stream, X, kept.codes, kept.exponents):
+        _check(load_library().mixgcn_checkpoint_unpack(
+            _dtype_of(X), _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents), _ld(kept.exponents), n, cols, _ptr(X),
+            _ld(X), _stream(stream)), "checkpoint_unpack")
+
+
+def checkpoint_wgrad_workspace(n: int, k: int, m: int) -> int:
+    """Bytes of workspace of checkpoint_wgrad."""
+    return load_library().mixgcn_checkpoint_wgrad_workspace(n, k, m)
+
+
+def checkpoint_wgrad(kept: Checkpoint, G, dW, mask=None, beta: float = 0.0, workspace=None, stream=None) -> None:
+    """dW = beta dW + Z^T (G (.) M) with Z the values of a checkpoint; mask: bitmap of G's shape (relu_bitmap)."""
+    n, k = kept.shape
+    m = G.shape[1]
+    _shape("G", G, n, m)
+    _shape("dW", dW, k, m, dtype=torch.float32)
+    if mask is not None and (mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2 or mask.shape[0] != n or
+                             mask.shape[1] < (m + 31) // 32 or mask.stride(1) != 1):
+        raise ValueError("mask: int32 [n, ceil(m / 32)] expected")
+    with _on(stream, G, kept.codes, kept.exponents, dW, mask) as on:
+        ws = on.workspace(workspace, checkpoint_wgrad_workspace(n, k, m))
+        _check(load_library().mixgcn_checkpoint_wgrad(
+            _dtype_of(G), _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents), _ld(kept.exponents), _ptr(G), _ld(G),
+            _ptr(dW), _ld(dW), n, k, m, _ptr(mask), mask.stride(0) if mask is not None else 0, beta, _ptr(ws), _nbytes(ws),
+            _stream(stream)), "checkpoint_wgrad")

@@ -137,6 +137,10 @@ void Timer::destroy()
 
 namespace {
 
+// most rows, features and classes of mixgcn_linear_xent: its grids and row numbers are 32 bits
+constexpr int64_t kMostXentRows = (int64_t)1 << 30;
+constexpr int32_t kMostXentFeatures = 1 << 16, kMostXentClasses = 1 << 24;
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int elem_size(int dtype) { return dtype == MIXGCN_BF16 ? 2 : 4; }
@@ -545,6 +549,105 @@ int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
         return fail(MIXGCN_EINVAL, "softmax_xent: sizes");
     return launch_softmax_xent(dtype, logits, ldl, labels, n, n_classes, dlogits, ldd, loss,
                                (hipStream_t)stream);
+}
+
+int64_t mixgcn_linear_xent_workspace(int dtype, int64_t n, int32_t k, int32_t n_classes, int gradients)
+{
+    if ((dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) || n < 0 || n > kMostXentRows || k <= 0 || k > kMostXentFeatures ||
+        n_classes <= 0 || n_classes > kMostXentClasses)
+        return -1;
+    return linear_xent_bytes(dtype, n, k, n_classes, gradients != 0);
+}
+
+int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, int64_t ldw, const int32_t* labels,
+                       int64_t n, int32_t k, int32_t n_classes, double* loss, float* row_loss, void* dH, int64_t ldd,
+                       float* dW, int64_t ldg, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) return fail(MIXGCN_EINVAL, "linear_xent: dtype");
+    if (n < 0 || k <= 0 || n_classes <= 0) return fail(MIXGCN_EINVAL, "linear_xent: sizes");
+    if (n > kMostXentRows || k > kMostXentFeatures || n_classes > kMostXentClasses)
+        return fail(MIXGCN_EUNSUPPORTED, "linear_xent: more than 2^30 rows, 2^16 features or 2^24 classes");
+    if (!loss && !row_loss && !dH && !dW) return fail(MIXGCN_EINVAL, "linear_xent: nothing to compute");
+    const int es = elem_size(dtype);
+    if (n > 0) {
+        if (!labels) return fail(MIXGCN_EINVAL, "linear_xent: labels are null");
+        MIXGCN_TRY(check_matrix("linear_xent: H", H, ldh, k, es));
+        if (dH) MIXGCN_TRY(check_matrix("linear_xent: dH", dH, ldd, k, es));
+        if (dH == H && ldd != ldh) return fail(MIXGCN_EINVAL, "linear_xent: dH over H needs H's leading dimension");
+    }
+    MIXGCN_TRY(check_matrix("linear_xent: W", W, ldw, n_classes, 4));
+    if (dW) MIXGCN_TRY(check_matrix("linear_xent: dW", dW, ldg, n_classes, 4));
+    if (dW == W) return fail(MIXGCN_EINVAL, "linear_xent: dW must not be W");
+    if (!workspace || (uintptr_t)workspace % 256 != 0)
+        return fail(MIXGCN_EINVAL, "linear_xent: workspace is null or not 256-byte aligned");
+    if (workspace_bytes < linear_xent_bytes(dtype, n, k, n_classes, dH || dW))
+        return fail(MIXGCN_EINVAL, "linear_xent: workspace smaller than mixgcn_linear_xent_workspace");
+    return launch_linear_xent(dtype, H, ldh, W, ldw, labels, n, k, n_classes, loss, row_loss, dH, ldd, dW, ldg, workspace,
+                              (hipStream_t)stream);
+}
+
+static int check_checkpoint(const char* what, const int8_t* codes, int64_t ld_codes, const uint8_t* exponents,
+                            int64_t ld_exponents, int64_t n_rows, int32_t n_cols)
+{
+    const std::string who(what);
+    if (n_rows < 0 || n_cols <= 0) return fail(MIXGCN_EINVAL, who + ": sizes");
+    if (n_rows == 0) return MIXGCN_OK;
+    MIXGCN_TRY(check_matrix((who + ": codes").c_str(), codes, ld_codes, n_cols, 1));
+    if (!exponents) return fail(MIXGCN_EINVAL, who + ": exponents: null pointer");
+    if (ld_exponents < ((int64_t)n_cols + 31) / 32)
+        return fail(MIXGCN_EINVAL, who + ": ld_exponents shorter than ceil(n_cols / 32)");
+    return MIXGCN_OK;
+}
+
+int mixgcn_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n_rows, int32_t n_cols, int8_t* codes,
+                           int64_t ld_codes, uint8_t* exponents, int64_t ld_exponents, void* stream)
+{
+    if (dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) return fail(MIXGCN_EINVAL, "checkpoint_pack: dtype");
+    MIXGCN_TRY(check_checkpoint("checkpoint_pack", codes, ld_codes, exponents, ld_exponents, n_rows, n_cols));
+    if (n_rows == 0) return MIXGCN_OK;
+    MIXGCN_TRY(check_matrix("checkpoint_pack: X", X, ldx, n_cols, elem_size(dtype)));
+    return launch_checkpoint_pack(dtype, X, ldx, n_rows, n_cols, codes, ld_codes, exponents, ld_exponents,
+                                  (hipStream_t)stream);
+}
+
+int mixgcn_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ld_codes, const uint8_t* exponents,
+                             int64_t ld_exponents, int64_t n_rows, int32_t n_cols, void* X, int64_t ldx, void* stream)
+{
+    if (dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) return fail(MIXGCN_EINVAL, "checkpoint_unpack: dtype");
+    MIXGCN_TRY(check_checkpoint("checkpoint_unpack", codes, ld_codes, exponents, ld_exponents, n_rows, n_cols));
+    if (n_rows == 0) return MIXGCN_OK;
+    MIXGCN_TRY(check_matrix("checkpoint_unpack: X", X, ldx, n_cols, elem_size(dtype)));
+    return launch_checkpoint_unpack(dtype, codes, ld_codes, exponents, ld_exponents, n_rows, n_cols, X, ldx,
+                                    (hipStream_t)stream);
+}
+
+int64_t mixgcn_checkpoint_wgrad_workspace(int64_t n_rows, int32_t k, int32_t m)
+{
+    if (n_rows < 0 || k <= 0 || m <= 0) return -1;
+    return checkpoint_wgrad_bytes(n_rows, k, m);
+}
+
+int mixgcn_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ld_codes, const uint8_t* exponents,
+                            int64_t ld_exponents, const void* G, int64_t ldg, float* dW, int64_t ldw, int64_t n_rows,
+                            int32_t k, int32_t m, const uint32_t* mask, int64_t ld_mask, float beta, void* workspace,
+                            int64_t workspace_bytes, void* stream)
+{
+    if (dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) return fail(MIXGCN_EINVAL, "checkpoint_wgrad: dtype");
+    if (beta != 0.f && beta != 1.f) return fail(MIXGCN_EINVAL, "checkpoint_wgrad: beta must be 0 or 1");
+    if (m <= 0) return fail(MIXGCN_EINVAL, "checkpoint_wgrad: sizes");
+    MIXGCN_TRY(check_checkpoint("checkpoint_wgrad", codes, ld_codes, exponents, ld_exponents, n_rows, k));
+    if (n_rows > 0) {
+        MIXGCN_TRY(check_matrix("checkpoint_wgrad: G", G, ldg, m, elem_size(dtype)));
+        if (mask && ld_mask < ((int64_t)m + 31) / 32)
+            return fail(MIXGCN_EINVAL, "checkpoint_wgrad: ld_mask shorter than ceil(m / 32) words");
+    }
+    MIXGCN_TRY(check_matrix("checkpoint_wgrad: dW", dW, ldw, m, 4));
+    if (!workspace || !aligned16(workspace))
+        return fail(MIXGCN_EINVAL, "checkpoint_wgrad: workspace is null or not 16-byte aligned");
+    if (workspace_bytes < checkpoint_wgrad_bytes(n_rows, k, m))
+        return fail(MIXGCN_EINVAL, "checkpoint_wgrad: workspace smaller than mixgcn_checkpoint_wgrad_workspace");
+    return launch_checkpoint_wgrad(dtype, codes, ld_codes, exponents, ld_exponents, G, ldg, dW, ldw, n_rows, k, m, mask,
+                                   ld_mask, beta, (float*)workspace, (hipStream_t)stream);
 }
 
 int mixgcn_stream_create_cu_subset(int lo, int hi, int groups, void** stream)

@@ -331,4 +331,20 @@ int launch_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
                         int64_t n, int32_t c, void* dlogits, int64_t ldd, double* loss,
                         hipStream_t s);
 
+// Loss of a linear last layer without its logits (linear_xent.hip); loss, row_loss, dH and dW are optional.
+int64_t linear_xent_bytes(int dtype, int64_t n, int32_t k, int32_t c, bool gradients);
+int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, int64_t ldw, const int32_t* labels,
+                       int64_t n, int32_t k, int32_t c, double* loss, float* row_loss, void* dH, int64_t ldd, float* dW,
+                       int64_t ldg, void* workspace, hipStream_t s);
+
+// Activations in 8 bits (checkpoint.hip)
+int launch_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n, int32_t cols, int8_t* codes, int64_t ldq,
+                           uint8_t* steps, int64_t lde, hipStream_t s);
+int launch_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ldq, const uint8_t* steps, int64_t lde, int64_t n,
+                             int32_t cols, void* X, int64_t ldx, hipStream_t s);
+int64_t checkpoint_wgrad_bytes(int64_t n, int32_t k, int32_t m);
+int launch_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ldq, const uint8_t* steps, int64_t lde,
+                            const void* G, int64_t ldg, float* dW, int64_t ldw, int64_t n, int32_t k, int32_t m,
+                            const uint32_t* mask, int64_t ldm, float beta, float* P, hipStream_t s);
+
 }  // namespace mixgcn

@@ -1,0 +1,285 @@
+"""Activations in 8 bits: the codes against their definition, bit for bit, and the weight gradient that reads them
+against 64 bits."""
+import pytest
+
+from parity import say
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def mg():
+    import paper_2501_01951_amd as m
+
+    m.load_library()
+    return m
+
+
+def matrix(rows, cols, dtype, fill=NAN):
+    per = 16 // torch.empty(0, dtype=dtype).element_size()
+    return torch.full((rows, (cols + per - 1) // per * per + per), fill, device="cuda", dtype=dtype)
+
+
+def values(n, cols, dtype, seed):
+    """Normal values of every scale that the format has, zeros, and groups of zeros."""
+    gen = torch.Generator(device="cuda").manual_seed(seed + 13 * n + cols)
+    x = matrix(n, cols, dtype)
+    e = torch.randint(-30, 30, (n, (cols + 31) // 32), device="cuda", generator=gen).double()
+    wild = torch.rand(e.shape, device="cuda", generator=gen) < 0.3
+    e = torch.where(wild, torch.randint(-150, 127, e.shape, device="cuda", generator=gen).double(), e)
+    v = torch.randn(n, cols, device="cuda", generator=gen, dtype=torch.float64).clamp_(-1.9, 1.9)
+    v *= torch.exp2(e).repeat_interleave(32, 1)[:, :cols]
+    v[torch.rand(v.shape, device="cuda", generator=gen) < 0.1] = 0
+    v[:, :32][torch.rand(n, device="cuda", generator=gen) < 0.1] = 0
+    x[:, :cols] = v.to(dtype)
+    return x[:, :cols]
+
+
+def table():
+    return torch.tensor([2.0 ** e for e in range(-133, 123)], device="cuda", dtype=torch.float64)
+
+
+def packed(x):
+    """(codes, exponents) from the definition, in 64 bits, group by group."""
+    n, cols = x.shape
+    powers = table()
+    codes = torch.empty(n, cols, device="cuda", dtype=torch.float64)
+    exps = torch.empty(n, (cols + 31) // 32, device="cuda", dtype=torch.int64)
+    for g in range(exps.shape[1]):
+        v = x[:, 32 * g:32 * g + 32].double()
+        top = torch.where(v.isfinite(), v.abs(), 0.0).amax(1)
+        # the first of the powers at which the largest is rounded to 127 at most
+        fits = torch.round(top[:, None] / powers) <= 127
+        exps[:, g] = fits.int().argmax(1)
+        codes[:, 32 * g:32 * g + 32] = torch.where(v.isfinite(), torch.round(v / powers[exps[:, g]][:, None]), -128.0)
+    return codes, exps
+
+
+def decoded(codes, exps):
+    z = codes.double() * table()[exps.long()].repeat_interleave(32, 1)[:, :codes.shape[1]]
+    return torch.where(codes.double() == -128, NAN, z)
+
+
+SIZES = [(1, 1), (1, 32), (2, 31), (3, 33), (7, 100), (4096, 64), (999, 602), (100003, 47), (5, 20000), (33, 1000), (2049, 256),
+         (70000, 130)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,cols", SIZES)
+def test_pack_and_unpack(mg, n, cols, dtype):
+    say(f"checkpoint n={n} cols={cols} {dtype}")
+    x = values(n, cols, DTYPES[dtype], 1)
+    if n > 2:
+        x[1, cols // 2], x[2, 0] = INF, NAN
+    pitch = (cols + 15) // 16 * 16 + 16
+    codes = torch.full((n, pitch), 99, device="cuda", dtype=torch.int8)
+    exps = torch.full((n, (cols + 31) // 32 + 1), 77, device="cuda", dtype=torch.uint8)
+    kept = mg.Checkpoint(codes[:, :cols], exps[:, :-1])
+    mg.checkpoint_pack(x, kept)
+    torch.cuda.synchronize()
+    want_codes, want_exps = packed(x)
+    assert torch.equal(kept.exponents.long(), want_exps)
+    assert torch.equal(kept.codes.double(), want_codes)
+    assert (exps[:, -1] == 77).all() and (codes[:, (cols + 15) // 16 * 16:] == 99).all()
+    assert (codes[:, cols:(cols + 15) // 16 * 16] == 0).all()
+    # both types: a value is a bf16 number
+    z = decoded(want_codes, want_exps)
+    for out in ("f32", "bf16"):
+        back = matrix(n, cols, DTYPES[out], 3.0)
+        mg.checkpoint_unpack(kept, back[:, :cols])
+        torch.cuda.synchronize()
+        assert torch.equal(back[:, :cols].double().nan_to_num(nan=1e300), z.nan_to_num(nan=1e300))
+        assert (back[:, cols:] == 3).all()
+    fine = x.isfinite().all(1)
+    step = table()[want_exps].repeat_interleave(32, 1)[:, :cols]
+    assert ((x.double() - z).abs() <= step / 2)[fine].all()
+
+
+def test_borders_of_a_step(mg):
+    """Largest magnitudes at and beside those where the step changes, and ties between codes."""
+    tops = [127.0, 127.25, 127.49999, 127.5, 127.5001, 127.99999, 128.0, 63.99999, 64.0, 1.0, 2.0 ** -149, 2.0 ** -133, 2.0 ** -127,
+            127.5 * 2.0 ** -133, 2.0 ** -126, 3.4028234663852886e38, 2.0 ** 127, 127.4 * 2.0 ** 121, 127.5 * 2.0 ** 121]
+    x = torch.zeros(len(tops), 32, device="cuda")
+    for i, t in enumerate(tops):
+        x[i, 0] = t if i % 2 else -t
+        x[i, 1:] = torch.arange(1, 32, device="cuda") * (t / 127.5 / 2)
+    kept = mg.checkpoint_pack(x)
+    torch.cuda.synchronize()
+    codes, exps = packed(x)
+    assert torch.equal(kept.exponents.long(), exps) and torch.equal(kept.codes.double(), codes)
+    assert exps.min() == 0 and exps.max() == 255
+
+
+def test_rows_of_a_long_matrix(mg):
+    """Offsets beyond 2^31 elements and 2^32 bytes."""
+    n, cols = 1 << 16, 33000
+    x = torch.empty(n, cols, device="cuda", dtype=torch.bfloat16)
+    assert x.numel() > 1 << 31
+    x.zero_()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    for r in (0, n // 2, n - 2):
+        x[r:r + 2] = torch.randn(2, cols, device="cuda", generator=gen)
+    say("checkpoint 65536 x 33000")
+    kept = mg.checkpoint_pack(x)
+    back = torch.full_like(x, 1.0)
+    mg.checkpoint_unpack(kept, back)
+    torch.cuda.synchronize()
+    for r in (0, n // 2, n - 2):
+        codes, exps = packed(x[r:r + 2])
+        assert torch.equal(kept.codes[r:r + 2].double(), codes) and torch.equal(kept.exponents[r:r + 2].long(), exps)
+        assert torch.equal(back[r:r + 2].double(), decoded(codes, exps))
+    assert not back[2:n // 2].any() and not back[n // 2 + 2:n - 2].any()
+
+
+# ---- weight gradient ------------------------------------------------------------------------------
+
+def problem(n, k, m, dtype, seed=0, masked=True):
+    gen = torch.Generator(device="cuda").manual_seed(seed + n + 5 * k + 11 * m)
+    codes = torch.randint(-127, 128, (n, (k + 15) // 16 * 16), device="cuda", generator=gen, dtype=torch.int8)[:, :k]
+    exps = torch.randint(120, 136, (n, (k + 31) // 32), device="cuda", generator=gen, dtype=torch.uint8)
+    g = matrix(n, m, dtype)
+    g[:, :m] = torch.randn(n, m, device="cuda", generator=gen)
+    mask = None
+    if masked:
+        mask = torch.randint(-2 ** 31, 2 ** 31, (n, (m + 31) // 32 + 1), device="cuda", generator=gen).int()[:, :-1]
+    return codes, exps, g[:, :m], mask
+
+
+def bits(mask, m):
+    j = torch.arange(m, device="cuda")
+    return ((mask[:, j // 32] >> (j % 32).int()) & 1).bool()
+
+
+def reference(codes, exps, g, mask):
+    z = decoded(codes, exps)
+    u = g.double() if mask is None else torch.where(bits(mask, g.shape[1]), g.double(), 0.0)
+    zt = z.t().contiguous()
+    return zt @ u, zt.abs() @ u.abs()
+
+
+def check(got, ref, mag, n, dtype, what, base=0.0):
+    """A value of the checkpoint and a bf16 gradient enter exactly, an fp32 one as the exact sum of three terms; the
+    sums of a slab of at most 1024 rows are fp32, three products to a step of 16 rows, each cut to 2^-23 of
+    the running sum, which is at most that of |a| |b|; slabs are joined in 64 bits and rounded once."""
+    steps = (3 if dtype == torch.float32 else 1) * (min(n, 4096) // 16 + 1)
+    off = mag * ((steps + 2) * 2.0 ** -23) + ref.abs() * 2.0 ** -24
+    bad = ~((got.double() - ref).abs() <= off)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+WGRADS = [(1, 1, 1), (1, 32, 4), (15, 33, 31), (16, 128, 128), (17, 129, 130), (33, 100, 47), (1000, 64, 32), (4096, 64, 32),
+          (20011, 200, 72), (5000, 602, 41), (300, 16, 1030), (40000, 256, 256)]
+
+
+@pytest.mark.parametrize("masked", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,m", WGRADS)
+def test_weight_gradient(mg, n, k, m, dtype, masked):
+    say(f"checkpoint_wgrad n={n} k={k} m={m} {dtype} masked={masked}")
+    codes, exps, g, mask = problem(n, k, m, DTYPES[dtype], masked=masked)
+    if masked:
+        # what a masked element holds does not matter
+        g[~bits(mask, m)] = NAN
+    kept = mg.Checkpoint(codes, exps)
+    need = mg.checkpoint_wgrad_workspace(n, k, m)
+    room = torch.full((need + 4096,), 255, device="cuda", dtype=torch.uint8)
+    dw = matrix(k, m, torch.float32, 5.0)
+    mg.checkpoint_wgrad(kept, g, dw[:, :m], mask=mask, workspace=room[:need])
+    torch.cuda.synchronize()
+    ref, mag = reference(codes, exps, g, mask)
+    check(dw[:, :m], ref, mag, n, DTYPES[dtype], "dW")
+    assert (dw[:, m:] == 5).all() and (room[need:] == 255).all()
+    # added to what is there: one more rounding
+    before = torch.randn(k, m, device="cuda")
+    dw[:, :m] = before
+    mg.checkpoint_wgrad(kept, g, dw[:, :m], mask=mask, beta=1.0)
+    torch.cuda.synchronize()
+    check(dw[:, :m], ref + before.double(), mag + before.double().abs(), n, DTYPES[dtype], "dW + beta")
+
+
+def test_without_rows(mg):
+    dw = torch.full((40, 8), 7.0, device="cuda")
+    kept = mg.Checkpoint.empty(0, 40)
+    g = torch.empty(0, 8, device="cuda")
+    mg.checkpoint_wgrad(kept, g, dw, beta=1.0)
+    torch.cuda.synchronize()
+    assert (dw == 7).all()
+    mg.checkpoint_wgrad(kept, g, dw)
+    torch.cuda.synchronize()
+    assert (dw == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_codes_of_what_was_not_finite(mg, dtype):
+    """A NaN in the activations is one in its feature's row of dW, and infinities in the gradient reach their column
+    as in fp32; nothing else does."""
+    say(f"checkpoint_wgrad not finite {dtype}")
+    n, k, m = 500, 70, 40
+    codes, exps, g, _ = problem(n, k, m, DTYPES[dtype], masked=False)
+    codes[77, 13] = -128
+    codes[:, 5] = codes[:, 5].clamp(min=1)
+    g[100, 9], g[200, 21] = INF, NAN
+    dw = torch.zeros(k, m, device="cuda")
+    mg.checkpoint_wgrad(mg.Checkpoint(codes, exps), g, dw)
+    torch.cuda.synchronize()
+    assert dw[13].isnan().all() and dw[:, 21].isnan().all() and dw[5, 9] == INF
+    keep = torch.ones(k, m, device="cuda", dtype=torch.bool)
+    keep[13], keep[:, 9], keep[:, 21] = False, False, False
+    codes[77, 13], g[100, 9], g[200, 21] = 0, 0, 0
+    ref, mag = reference(codes, exps, g, None)
+    check(torch.where(keep, dw, 0), torch.where(keep, ref, 0), mag, n, DTYPES[dtype], "dW")
+    # an infinity times a code of either sign, or zero
+    col = decoded(codes, exps)[100]
+    want = torch.where(col > 0, INF, torch.where(col < 0, -INF, NAN)).float()
+    want[13] = NAN
+    assert torch.equal(dw[:, 9].nan_to_num(nan=1.0), want.nan_to_num(nan=1.0))
+
+
+@pytest.mark.parametrize("scale", [1e-37, 1e-30, 1e30])
+def test_gradients_of_every_magnitude(mg, scale):
+    say(f"checkpoint_wgrad scale {scale}")
+    codes, exps, g, _ = problem(700, 64, 48, torch.float32, masked=False)
+    g.mul_(scale)
+    if scale < 1:
+        exps.add_(60)  # products of normal size
+    dw = torch.zeros(64, 48, device="cuda")
+    mg.checkpoint_wgrad(mg.Checkpoint(codes, exps), g, dw)
+    torch.cuda.synchronize()
+    ref, mag = reference(codes, exps, g, None)
+    check(dw, ref, mag, 700, torch.float32, "dW")
+
+
+def test_same_bits_streams_and_graphs(mg):
+    codes, exps, g, mask = problem(30000, 150, 90, torch.float32)
+    kept = mg.Checkpoint(codes, exps)
+    want = torch.zeros(150, 92, device="cuda")[:, :90]
+    mg.checkpoint_wgrad(kept, g, want, mask=mask)
+    outs = [torch.zeros(150, 92, device="cuda")[:, :90] for _ in range(2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    say("checkpoint_wgrad on two streams")
+    for _ in range(3):
+        for o, s in zip(outs, streams):
+            mg.checkpoint_wgrad(kept, g, o, mask=mask, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    say("checkpoint captured")
+    x = torch.randn(30000, 150, device="cuda")
+    x = torch.nn.functional.pad(x, (0, 2))[:, :150]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mg.checkpoint_pack(x, kept)
+        mg.checkpoint_wgrad(kept, g, outs[0], mask=mask)
+    for _ in range(3):
+        x.mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.zeros(150, 92, device="cuda")[:, :90]
+        mg.checkpoint_wgrad(mg.checkpoint_pack(x), g, eager, mask=mask)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], eager)
