@@ -420,7 +420,7 @@ int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
  *   workspace : device memory of mixgcn_linear_xent_workspace(...) bytes, 256-byte aligned, which the call uses
  *   until its work on the stream is done (calls that overlap need one each).  The call allocates nothing and does
  *   not synchronise.  mixgcn_linear_xent_workspace (host arithmetic; gradients: whether dH or dW is wanted) is -1
- *   for bad sizes: at most 2^30 rows, 2^16 features, 2^24 classes.
+ *   for bad sizes: at most 2^30 rows, 2^16 features, 2^22 classes.
  */
 int64_t mixgcn_linear_xent_workspace(int dtype, int64_t n, int32_t k, int32_t n_classes, int gradients);
 int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, int64_t ldw, const int32_t* labels,

@@ -137,9 +137,9 @@ void Timer::destroy()
 
 namespace {
 
-// most rows, features and classes of mixgcn_linear_xent: its grids and row numbers are 32 bits
+// most rows, features and classes of mixgcn_linear_xent: its grids, row numbers and offsets within a tile are 32 bits
 constexpr int64_t kMostXentRows = (int64_t)1 << 30;
-constexpr int32_t kMostXentFeatures = 1 << 16, kMostXentClasses = 1 << 24;
+constexpr int32_t kMostXentFeatures = 1 << 16, kMostXentClasses = 1 << 22;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -566,7 +566,7 @@ int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     if (dtype != MIXGCN_F32 && dtype != MIXGCN_BF16) return fail(MIXGCN_EINVAL, "linear_xent: dtype");
     if (n < 0 || k <= 0 || n_classes <= 0) return fail(MIXGCN_EINVAL, "linear_xent: sizes");
     if (n > kMostXentRows || k > kMostXentFeatures || n_classes > kMostXentClasses)
-        return fail(MIXGCN_EUNSUPPORTED, "linear_xent: more than 2^30 rows, 2^16 features or 2^24 classes");
+        return fail(MIXGCN_EUNSUPPORTED, "linear_xent: more than 2^30 rows, 2^16 features or 2^22 classes");
     if (!loss && !row_loss && !dH && !dW) return fail(MIXGCN_EINVAL, "linear_xent: nothing to compute");
     const int es = elem_size(dtype);
     if (n > 0) {

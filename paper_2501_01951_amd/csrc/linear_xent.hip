@@ -31,10 +31,10 @@ typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 typedef __attribute__((address_space(3))) uintx4 lds_uintx4;
 
-constexpr int kTile = 128;        // rows, classes and features of a tile
+constexpr int kTile = 128;        // classes and features of a tile
+constexpr int kMostTileRows = 256;  // rows of the largest tile
 constexpr int kHalfTile = 64;     // classes of a partial sum: what a wavefront holds
 constexpr int BK = 32;            // reduction depth of a step
-constexpr int kListRows = 4096;   // labels of a block of the list kernels
 constexpr float kGradScale = 32768.f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
@@ -48,14 +48,24 @@ struct Meta {
 
 __device__ inline bool has_label(int32_t y, int32_t c) { return (uint32_t)y < (uint32_t)c; }
 
+constexpr int kListStep = 4 * kBlock;  // labels that a block looks at at a time, four per thread
+
+__device__ inline uint32_t labelled4(const int32_t* labels, int64_t r, int64_t end, int32_t c)
+{
+    uint32_t have = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (r + i < end && has_label(labels[r + i], c)) have |= 1u << i;
+    return have;
+}
+
 __global__ __launch_bounds__(kBlock) void count_labels_kernel(const int32_t* __restrict__ labels, int64_t n, int32_t c,
-                                                              uint32_t* __restrict__ counts)
+                                                              int per_block, uint32_t* __restrict__ counts)
 {
     __shared__ uint32_t part[kBlock / kWave];
-    const int64_t r0 = (int64_t)blockIdx.x * kListRows;
+    const int64_t r0 = (int64_t)blockIdx.x * per_block, end = r0 + per_block < n ? r0 + per_block : n;
     uint32_t mine = 0;
-    for (int i = threadIdx.x; i < kListRows; i += kBlock)
-        if (r0 + i < n && has_label(labels[r0 + i], c)) ++mine;
+    for (int64_t r = r0 + 4 * threadIdx.x; r < end; r += kListStep) mine += __popc(labelled4(labels, r, end, c));
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, kWave);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
@@ -63,29 +73,30 @@ __global__ __launch_bounds__(kBlock) void count_labels_kernel(const int32_t* __r
     if (threadIdx.x == 0) counts[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
-// rows[i]: the i-th row with a label.  Clears the maxima of the features, too.
+// rows[i]: the i-th row with a label.  Clears the maxima of the features.
 __global__ __launch_bounds__(kBlock) void list_labels_kernel(const int32_t* __restrict__ labels, int64_t n, int32_t c,
-                                                             const uint32_t* __restrict__ counts, uint32_t* __restrict__ rows,
-                                                             Meta* __restrict__ meta, uint32_t* __restrict__ top, int n_top)
+                                                             int per_block, const uint32_t* __restrict__ counts,
+                                                             uint32_t* __restrict__ rows, Meta* __restrict__ meta,
+                                                             uint32_t* __restrict__ top, int n_top)
 {
     __shared__ uint64_t lds[4];
     const int tid = threadIdx.x;
     uint64_t before = 0;
     for (unsigned b = tid; b < blockIdx.x; b += kBlock) before += counts[b];
-    uint64_t base;
-    block_exclusive_scan_u64(before, &base, lds);
-    constexpr int PER = kListRows / kBlock;
-    const int64_t r0 = (int64_t)blockIdx.x * kListRows + tid * PER;
-    uint32_t have = 0;
+    uint64_t base = 0;
+    if (blockIdx.x > 0) block_exclusive_scan_u64(before, &base, lds);
+    const int64_t r0 = (int64_t)blockIdx.x * per_block, end = r0 + per_block < n ? r0 + per_block : n;
+    for (int64_t s = r0; s < end; s += kListStep) {
+        const int64_t r = s + 4 * tid;
+        const uint32_t have = labelled4(labels, r, end, c);
+        uint64_t total;
+        uint64_t at = base + block_exclusive_scan_u64(__popc(have), &total, lds);
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (r0 + i < n && has_label(labels[r0 + i], c)) have |= 1u << i;
-    uint64_t total;
-    uint64_t at = base + block_exclusive_scan_u64(__popc(have), &total, lds);
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (have >> i & 1u) rows[at++] = (uint32_t)(r0 + i);
-    if (blockIdx.x == gridDim.x - 1 && tid == 0) meta->count = (uint32_t)(base + total);
+        for (int i = 0; i < 4; ++i)
+            if (have >> i & 1u) rows[at++] = (uint32_t)(r + i);
+        base += total;
+    }
+    if (blockIdx.x == gridDim.x - 1 && tid == 0) meta->count = (uint32_t)base;
     if (blockIdx.x == 0)
         for (int i = tid; i < n_top; i += kBlock) top[i] = 0u;
 }
@@ -93,57 +104,32 @@ __global__ __launch_bounds__(kBlock) void list_labels_kernel(const int32_t* __re
 // ---- scales -------------------------------------------------------------------------------------
 
 template <bool BF16>
-__device__ inline float feature(const void* p, int64_t i)
-{
-    return BF16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16) : ((const float*)p)[i];
-}
+struct Eight {  // eight features of a row; the row's pitch holds whole 16 bytes
+    static constexpr int V = BF16 ? 1 : 2;
+    uint4 v[V];
+    __device__ inline void load(const void* p, int64_t row_at, int j, int64_t ld)
+    {
+        if (BF16) {
+            v[0] = *reinterpret_cast<const uint4*>((const uint16_t*)p + row_at + j);
+        } else {
+            v[0] = *reinterpret_cast<const uint4*>((const float*)p + row_at + j);
+            v[V - 1] = *reinterpret_cast<const uint4*>((const float*)p + row_at + (j + 4 < ld ? j + 4 : j));
+        }
+    }
+    __device__ inline float get(int e) const
+    {
+        const uint4 q = v[BF16 ? 0 : e / 4];
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        if (BF16) return e & 1 ? high_half(w[e / 2]) : low_half(w[e / 2]);
+        return __uint_as_float(w[e % 4]);
+    }
+};
 // magnitude as an integer, 0 of what is not finite
 __device__ inline uint32_t magnitude(float x)
 {
     const uint32_t m = __float_as_uint(x) & 0x7FFFFFFFu;
     return m < 0x7F800000u ? m : 0u;
 }
-
-constexpr int kMaxCols = 4096;    // columns of a row of W per block
-
-// top[k]: largest magnitude of column k of H over the rows with a label; top[kp + k]: of row k of W.  (Maxima do not
-// depend on the order of the atomics.)
-template <bool BF16>
-__global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H, int64_t ldh,
-                                                     const uint32_t* __restrict__ rows, const Meta* __restrict__ meta,
-                                                     const float* __restrict__ W, int64_t ldw, int k, int c, int kp,
-                                                     int w_blocks, int w_pieces, int h_rows, uint32_t* __restrict__ top)
-{
-    if ((int)blockIdx.x < w_blocks) {
-        const int row = blockIdx.x / w_pieces, c0 = (int)(blockIdx.x % w_pieces) * kMaxCols;
-        const int c1 = c - c0 < kMaxCols ? c : c0 + kMaxCols;
-        uint32_t m = 0;
-        for (int j = c0 + threadIdx.x; j < c1; j += kBlock) {
-            const uint32_t t = magnitude(W[(int64_t)row * ldw + j]);
-            m = t > m ? t : m;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint32_t t = __shfl_xor(m, o, kWave);
-            m = t > m ? t : m;
-        }
-        if ((threadIdx.x & 63) == 0) atomicMax(top + kp + row, m);
-        return;
-    }
-    const uint32_t count = meta->count;
-    const uint32_t i0 = (blockIdx.x - w_blocks) * (uint32_t)h_rows;
-    if (i0 >= count) return;
-    const int m_rows = count - i0 < (uint32_t)h_rows ? (int)(count - i0) : h_rows;
-    for (int j = threadIdx.x; j < k; j += kBlock) {
-        uint32_t m = 0;
-        for (int i = 0; i < m_rows; ++i) {
-            const uint32_t t = magnitude(feature<BF16>(H, (int64_t)rows[i0 + i] * ldh + j));
-            m = t > m ? t : m;
-        }
-        atomicMax(top + j, m);
-    }
-}
-
 __device__ inline int exponent_of(uint32_t bits)
 {
     int e;
@@ -151,17 +137,17 @@ __device__ inline int exponent_of(uint32_t bits)
     return e - 1;
 }
 
-// shift[k], shift[kp + k]: powers of two that feature k is taken times in H and in W.
-__global__ __launch_bounds__(kBlock) void scale_kernel(const uint32_t* __restrict__ top, int k, int kp,
-                                                       int32_t* __restrict__ shift, Meta* __restrict__ meta)
+// The exponent of the largest product of a feature's two magnitudes, for a whole block.
+__device__ inline int most_exponent(const uint32_t* __restrict__ top, int k, int kp, int* most_of)
 {
-    __shared__ int most_of[kBlock / kWave];
     int most = -1000;
-    for (int i = threadIdx.x; i < k; i += kBlock)
-        if (top[i] && top[kp + i]) {
-            const int e = exponent_of(top[i]) + exponent_of(top[kp + i]);
+    for (int i = threadIdx.x; i < k; i += kBlock) {
+        const uint32_t h = top[i], w = top[kp + i];
+        if (h && w) {
+            const int e = exponent_of(h) + exponent_of(w);
             most = e > most ? e : most;
         }
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         const int t = __shfl_xor(most, o, kWave);
@@ -171,25 +157,122 @@ __global__ __launch_bounds__(kBlock) void scale_kernel(const uint32_t* __restric
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kBlock / kWave; ++w) most = most_of[w] > most ? most_of[w] : most;
-    if (most == -1000) most = 28;      // all products are zero
-    if (most > 155) most = 155;        // larger logits are not finite: alpha is
-    for (int i = threadIdx.x; i < kp; i += kBlock) {
-        int sh = 0, sw = 0;
-        const bool h = i < k && top[i], w = i < k && top[kp + i];
-        if (h && w) {
-            const int eh = exponent_of(top[i]), ew = exponent_of(top[kp + i]);
-            const int both = eh + ew - most, half = both >> 1;
-            sh = 14 + half - eh;
-            sw = 14 + (both - half) - ew;
-        } else if (h) {
-            sh = 14 - exponent_of(top[i]);
-        } else if (w) {
-            sw = 14 - exponent_of(top[kp + i]);
+    if (most == -1000) most = 28;  // all products are zero
+    if (most > 155) most = 155;    // larger logits are not finite: alpha is
+    return most;
+}
+
+// The power of two that a feature is taken times on one side: `mine` is its largest magnitude there, `other` the one on
+// the other side.  `rest`: this side takes what is left over where their exponents cannot be shared evenly.
+__device__ inline int scale_of(uint32_t mine, uint32_t other, int most, bool rest = false)
+{
+    if (!mine) return 0;
+    const int e = exponent_of(mine);
+    if (!other) return 14 - e;
+    const int both = e + exponent_of(other) - most, half = both >> 1;
+    return 14 + (rest ? both - half : half) - e;
+}
+
+constexpr int kTopCols = 4096;  // columns of a row of W per block
+constexpr int kTopWidth = 8 * kBlock;  // columns of H that a block takes at a time
+
+// What the roles of the blocks of top_kernel are.
+struct TopPlan {
+    int w_blocks, w_pieces;   // maxima of the rows of W
+    int h_blocks, h_rows;     // maxima of the columns of H, h_rows listed rows to a block
+    int clear_blocks;         // zeros for the rows without a label
+};
+
+// top[k]: largest magnitude of column k of H over the rows with a label; top[kp + k]: of row k of W.  (Maxima do not
+// depend on the order of the atomics.)  And, beside that, zeros for the rows without a label, of dH (if it is given) and of
+// the losses of the rows.
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H, int64_t ldh,
+                                                     const uint32_t* __restrict__ rows, const Meta* __restrict__ meta,
+                                                     const float* __restrict__ W, int64_t ldw, int k, int c, int kp,
+                                                     TopPlan plan, uint32_t* __restrict__ top,
+                                                     const int32_t* __restrict__ labels, int64_t n, void* __restrict__ dH,
+                                                     int64_t ldd, float* __restrict__ row_loss)
+{
+    __shared__ uint32_t col_top[kTopWidth];
+    const int tid = threadIdx.x;
+    int b = blockIdx.x;
+    if (b < plan.w_blocks) {
+        const int row = b / plan.w_pieces, c0 = b % plan.w_pieces * kTopCols;
+        const float* const w = W + (int64_t)row * ldw;
+        float4 v[kTopCols / 4 / kBlock];
+#pragma unroll
+        for (int i = 0; i < kTopCols / 4 / kBlock; ++i) {
+            const int j = c0 + 4 * (tid + i * kBlock);
+            v[i] = *reinterpret_cast<const float4*>(w + (j < c ? j : c0));
         }
-        shift[i] = sh;
-        shift[kp + i] = sw;
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kTopCols / 4 / kBlock; ++i) {
+            const int j = c0 + 4 * (tid + i * kBlock);
+            const float f[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t t = j + e < c ? magnitude(f[e]) : 0u;
+                m = t > m ? t : m;
+            }
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const uint32_t t = __shfl_xor(m, o, kWave);
+            m = t > m ? t : m;
+        }
+        if ((tid & 63) == 0) atomicMax(top + kp + row, m);
+    } else if (b < plan.w_blocks + plan.h_blocks) {
+        const uint32_t count = meta->count, i0 = (uint32_t)(b - plan.w_blocks) * (uint32_t)plan.h_rows;
+        const int m_rows = i0 >= count ? 0 : count - i0 < (uint32_t)plan.h_rows ? (int)(count - i0) : plan.h_rows;
+        for (int j0 = 0; j0 < k && m_rows > 0; j0 += kTopWidth) {
+            const int width = k - j0 < kTopWidth ? k - j0 : kTopWidth;
+            const int lanes = (width + 7) / 8, at_once = kBlock / lanes;
+            for (int i = tid; i < width; i += kBlock) col_top[i] = 0u;
+            __syncthreads();
+            const int j = 8 * (tid % lanes);
+            uint32_t m[8] = {};
+            if (tid < at_once * lanes)
+                for (int i = tid / lanes; i < m_rows; i += at_once) {
+                    Eight<BF16> x;
+                    x.load(H, (int64_t)rows[i0 + i] * ldh, j0 + j, ldh);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t t = magnitude(x.get(e));
+                        m[e] = t > m[e] ? t : m[e];
+                    }
+                }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < width && m[e]) atomicMax(&col_top[j + e], m[e]);
+            __syncthreads();
+            for (int i = tid; i < width; i += kBlock) atomicMax(top + j0 + i, col_top[i]);
+            __syncthreads();
+        }
+    } else {
+        b -= plan.w_blocks + plan.h_blocks;
+        const int cols = dH ? k : 0, per_row = dH ? (k + 7) / 8 : 1;
+        const int64_t items = n * per_row;
+        for (int64_t it = (int64_t)b * kBlock + tid; it < items; it += (int64_t)plan.clear_blocks * kBlock) {
+            const int64_t r = it / per_row;
+            const int j = (int)(it - r * per_row) * 8;
+            if (has_label(labels[r], c)) continue;
+            if (j == 0 && row_loss) row_loss[r] = 0.f;
+            const int64_t at = r * ldd + j;
+            if (j + 8 <= cols) {
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                uint4* const o = reinterpret_cast<uint4*>((char*)dH + at * (BF16 ? 2 : 4));
+                o[0] = zero;
+                if (!BF16) o[1] = zero;
+            } else {
+                for (int e = 0; j + e < cols; ++e) {
+                    if (BF16) ((uint16_t*)dH)[at + e] = 0;
+                    else ((float*)dH)[at + e] = 0.f;
+                }
+            }
+        }
     }
-    if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most - 28);
 }
 
 // ---- operands as f16 terms ----------------------------------------------------------------------
@@ -221,208 +304,253 @@ __device__ inline float rest_of(float x, float t)
     return fabsf(t) <= 65504.f ? r : 0.f;
 }
 
-// planes[t][i][kp]: the scaled features of the listed rows [first, first + rows of the piece), zeros past the last one
-// up to a whole tile and past the features.  y[i]: their labels, -1 past the last one.
-template <bool BF16>
-__global__ __launch_bounds__(kBlock) void split_rows_kernel(const void* __restrict__ H, int64_t ldh,
-                                                            const uint32_t* __restrict__ rows,
-                                                            const int32_t* __restrict__ labels,
-                                                            const Meta* __restrict__ meta, uint32_t first, int piece_rows,
-                                                            int k, int kp, const int32_t* __restrict__ shift,
-                                                            uint16_t* __restrict__ planes, int32_t* __restrict__ y)
+constexpr int kScaleCols = 2048;  // features whose scales a block keeps in LDS (a multiple of 8)
+
+// The two terms of eight numbers to a plane and the next.
+__device__ inline void put_terms(uint16_t* o, size_t plane, const float (&x)[8], bool both)
 {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        hi[q] = pack_f16(x[2 * q], x[2 * q + 1]);
+        lo[q] = pack_f16(rest_of(x[2 * q], low_f16(hi[q])), rest_of(x[2 * q + 1], high_f16(hi[q])));
+    }
+    *reinterpret_cast<uint4*>(o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// planes[t]: the scaled features of the listed rows [first, first + rows of the piece), zeros past the last one up to a
+// whole tile and past the features.  y[i]: their labels, -1 past the last one.
+// The first w_blocks blocks: wplanes[t], the two terms of the scaled weights, rows the classes, columns the features,
+// zeros past them.
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ H, int64_t ldh,
+                                                       const uint32_t* __restrict__ rows,
+                                                       const int32_t* __restrict__ labels, Meta* __restrict__ meta,
+                                                       uint32_t first, int piece_rows, int h_rows, int k, int kp,
+                                                       const uint32_t* __restrict__ top, int32_t* __restrict__ shift,
+                                                       uint16_t* __restrict__ planes, int32_t* __restrict__ y, int w_blocks,
+                                                       const float* __restrict__ W, int64_t ldw, int c, int cp, int w_rows,
+                                                       uint16_t* __restrict__ wplanes)
+{
+    __shared__ int most_of[kBlock / kWave];
+    __shared__ int16_t scale_lds[kScaleCols];
+    const int most = most_exponent(top, k, kp, most_of);
+    if (blockIdx.x == 0) {
+        // for the kernels that follow
+        for (int i = threadIdx.x; i < kp; i += kBlock) {
+            shift[i] = scale_of(top[i], top[kp + i], most);
+            shift[kp + i] = scale_of(top[kp + i], top[i], most, true);
+        }
+        if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most - 28);
+    }
+    const bool weights = (int)blockIdx.x < w_blocks;
+    for (int i = threadIdx.x; i < k && i < kScaleCols; i += kBlock)
+        scale_lds[i] = (int16_t)(weights ? scale_of(top[kp + i], top[i], most, true) : scale_of(top[i], top[kp + i], most));
+    __syncthreads();
+    if (weights) {
+        // a thread takes 32 features of a class
+        const int64_t items = (int64_t)(kp / BK) * cp;
+        const size_t plane = (size_t)(kp / BK) * w_rows * BK;
+        for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)w_blocks * kBlock) {
+            const int b = (int)(it / cp), j = (int)(it - (int64_t)b * cp);
+            uint16_t* const o = wplanes + ((size_t)b * w_rows + j) * BK;
+            float x[BK];
+#pragma unroll
+            for (int e = 0; e < BK; ++e) x[e] = j < c && b * BK + e < k ? W[(int64_t)(b * BK + e) * ldw + j] : 0.f;
+#pragma unroll
+            for (int q = 0; q < BK / 8; ++q) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = b * BK + 8 * q + e;
+                    const int s = i >= k ? 0 : b * BK < kScaleCols ? scale_lds[i] : scale_of(top[kp + i], top[i], most, true);
+                    v[e] = ldexpf(x[8 * q + e], s);
+                }
+                put_terms(o + 8 * q, plane, v, true);
+            }
+        }
+        return;
+    }
     const uint32_t count = meta->count;
     if (first >= count) return;
     const int live = count - first < (uint32_t)piece_rows ? (int)(count - first) : piece_rows;
-    const int end = (live + kTile - 1) / kTile * kTile;
-    const int per_row = kp / 8;
-    const int64_t items = (int64_t)end * per_row;
-    const size_t plane = (size_t)piece_rows * kp;
-    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)gridDim.x * kBlock) {
-        const int i = (int)(it / per_row), j = (int)(it % per_row) * 8;
+    const int end = (live + kMostTileRows - 1) / kMostTileRows * kMostTileRows;
+    const size_t plane = (size_t)(kp / BK) * h_rows * BK;
+    // four threads take the 32 features of a block in a row
+    const int64_t items = (int64_t)end * (kp / 8), step = (int64_t)(gridDim.x - w_blocks) * kBlock;
+    for (int64_t it = (int64_t)(blockIdx.x - w_blocks) * kBlock + threadIdx.x; it < items; it += step) {
+        const int b = (int)(it / (4 * end)), at = (int)(it - (int64_t)b * (4 * end)), i = at / 4, j = b * BK + at % 4 * 8;
         const bool in = i < live;
         const uint32_t r = in ? rows[first + i] : 0u;
         if (j == 0) y[i] = in ? labels[r] : -1;
-        uint32_t hi[4], lo[4];
+        float x[8] = {};
+        if (in && j < k) {
+            Eight<BF16> v;
+            v.load(H, (int64_t)r * ldh, j, ldh);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float x[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int col = j + 2 * q + b;
-                x[b] = in && col < k ? ldexpf(feature<BF16>(H, (int64_t)r * ldh + col), shift[col]) : 0.f;
-            }
-            hi[q] = pack_f16(x[0], x[1]);
-            lo[q] = pack_f16(rest_of(x[0], low_f16(hi[q])), rest_of(x[1], high_f16(hi[q])));
+            for (int e = 0; e < 8; ++e)
+                if (j + e < k)
+                    x[e] = ldexpf(v.get(e), j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most));
         }
-        uint16_t* const o = planes + (size_t)i * kp + j;
-        *reinterpret_cast<uint4*>(o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        if (!BF16) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    }
-}
-
-// planes[t][k][cp]: the two terms of the scaled weights, zeros past them.
-__global__ __launch_bounds__(kBlock) void split_weights_kernel(const float* __restrict__ W, int64_t ldw, int k, int c,
-                                                               int kp, int cp, const int32_t* __restrict__ shift,
-                                                               uint16_t* __restrict__ planes)
-{
-    const int per_row = cp / 8;
-    const int64_t items = (int64_t)kp * per_row;
-    const size_t plane = (size_t)kp * cp;
-    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)gridDim.x * kBlock) {
-        const int i = (int)(it / per_row), j = (int)(it % per_row) * 8;
-        const int s = shift[kp + i];
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float x[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int col = j + 2 * q + b;
-                x[b] = i < k && col < c ? ldexpf(W[(int64_t)i * ldw + col], s) : 0.f;
-            }
-            hi[q] = pack_f16(x[0], x[1]);
-            lo[q] = pack_f16(rest_of(x[0], low_f16(hi[q])), rest_of(x[1], high_f16(hi[q])));
-        }
-        uint16_t* const o = planes + (size_t)i * cp + j;
-        *reinterpret_cast<uint4*>(o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        put_terms(planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8, plane, x, !BF16);
     }
 }
 
 // ---- a tile of a product ------------------------------------------------------------------------
-// 128 x 128 sums of A[i][k] B[k][j] on four wavefronts of 64 x 64, the operands as planes of f16 terms in memory that
-// holds whole tiles.  An operand lies either with the reduction index contiguous (rows of its free index) or, TR, with
-// the free index contiguous (rows of the reduction index); the transposing LDS read turns the latter: lane i of 16
-// receives element i % 4 of the 8 bytes that lanes i / 4, + 4, + 8 and + 12 address.
+// Operands lie in memory as planes of f16 terms in blocks of 32 columns: column j of row i is at
+// [j / 32][i][j % 32], with `rows` rows to a block.  A product takes one with the reduction along its columns (a step of
+// 32 is a block, tile rows times 64 contiguous bytes), or, TR, along its rows (a step is 32 rows of each of the tile's
+// blocks, 2 KB contiguous); the transposing LDS read turns the latter: lane i of 16 receives element i % 4 of the 8 bytes
+// that lanes i / 4, + 4, + 8 and + 12 address.  (With plain rows, of which a step takes 64 bytes each, the product
+// of 7800 x 7150 gradients and 7150 x 512 weights took 137 us.)
+//
+// Sums of A[i][k] B[k][j] over a tile of 64 TM x 64 TN, on 2 x 2 wavefronts of 32 TM x 32 TN.  Steps go straight from
+// memory to LDS, 16 bytes per lane and 1 KB per instruction, STAGES - 1 of them ahead; there is one barrier per step,
+// before which a wavefront waits for its own part of the step that is due and for what it has read.  LDS holds rows
+// without padding, so the 16-byte pieces of a row are put in another order, which each lane fetches from: rows of 64
+// bytes have piece p at p ^ (row / 4 % 4), and rows of the free index, in which the transposing read takes 64 bytes of
+// four rows at a time, the 64-byte block q at q ^ (row % 4).  Either way the lanes that are served together hit all
+// banks.
 struct Operand {
     const uint16_t* p;  // first term of the tile's first element
-    int64_t ld;         // halfwords from row to row
+    int64_t rows;       // rows of a block in memory
     size_t plane;       // halfwords from term to term
 };
 
-template <int TA, int TB, bool TRA, bool TRB>
-struct Product {
-    static constexpr int PITCH_N = BK + 8;      // 80 bytes: 16 rows of 16 bytes hit all banks
-    static constexpr int PITCH_T = kTile + 32;  // 320 bytes: four rows of 64 bytes, too
-    static constexpr int PLANE = kTile * PITCH_N;
-    static_assert(PLANE == BK * PITCH_T, "both layouts take the same room");
-    static constexpr int BUFFER = (TA + TB) * PLANE;   // halfwords
-    static constexpr int LDS = 2 * BUFFER;
+__device__ inline void clobber() { asm volatile("" ::: "memory"); }
+template <int N>
+__device__ inline void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    clobber();
+}
+// 16 bytes per lane from base + offset to LDS at lds + 16 lane (lds in bytes, the same for the wavefront).  The
+// compiler does not count this load: wait_and_meet waits for it.  (M0 is no register that the compiler keeps values in,
+// and nothing else here uses it.)
+__device__ inline void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+}
 
-    template <bool TR>
-    static __device__ inline int64_t source(int64_t ld, int piece)
+template <int TA, int TB, bool TRA, bool TRB, int TM, int TN, int STAGES>
+struct Product {
+    static constexpr int WA = 64 * TM, WB = 64 * TN;              // extents of the tile
+    static constexpr int PA = WA * BK, PB = WB * BK;              // halfwords of a plane
+    static constexpr int BUFFER = TA * PA + TB * PB;
+    static constexpr int LDS = STAGES * BUFFER;
+    static constexpr int IA = PA / 512 / 4, IB = PB / 512 / 4;    // loads of a wavefront per plane
+    static constexpr int LOADS = TA * IA + TB * IB;
+
+    // where lane `lane` of load `i` of a plane reads, in bytes from the plane's first element of the step
+    template <bool TR, int WIDTH>
+    static __device__ inline uint32_t source(int64_t rows, int i, int lane)
     {
-        return TR ? (int64_t)(piece / 16) * ld + 8 * (piece % 16) : (int64_t)(piece / 4) * ld + 8 * (piece % 4);
+        if (TR) {
+            const int row = (i * 64 + lane) / (WIDTH / 8), slot = (i * 64 + lane) % (WIDTH / 8);
+            return (uint32_t)((slot / 4 ^ (row & 3)) * rows * 64) + 64u * (uint32_t)row + 16u * (uint32_t)(slot % 4);
+        }
+        const int row = i * 16 + lane / 4, slot = lane % 4;
+        return 64u * (uint32_t)row + 16u * (uint32_t)(slot ^ ((row >> 2) & 3));
     }
-    template <bool TR>
-    static __device__ inline int place(int piece)
-    {
-        return TR ? (piece / 16) * PITCH_T + 8 * (piece % 16) : (piece / 4) * PITCH_N + 8 * (piece % 4);
-    }
-    template <bool TR>
+    // halfwords from the plane's start: operand of the 32 free indices from free0 on, 16 reduction indices from kc on
+    template <bool TR, int WIDTH>
     static __device__ inline half8 fragment(const uint16_t* t, int free0, int kc, int lane)
     {
         half8 o;
         if (TR) {
-            const int grp = lane >> 4, gs = lane & 15;
-            const uint16_t* const p = t + (kc + 8 * (grp >> 1) + (gs >> 2)) * PITCH_T + free0 + 16 * (grp & 1) + 4 * (gs & 3);
+            const int grp = lane >> 4, gs = lane & 15, row = kc + 8 * (grp >> 1) + (gs >> 2);
+            const uint16_t* const p = t + row * WIDTH + (((free0 / 32) ^ (row & 3)) * 32) + 16 * (grp & 1) + 4 * (gs & 3);
             const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)p);
-            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * PITCH_T));
+            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * WIDTH));
             const shortx8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             __builtin_memcpy(&o, &v, 16);
         } else {
-            o = *reinterpret_cast<const half8*>(t + (free0 + (lane & 31)) * PITCH_N + kc + 8 * (lane >> 5));
+            const int r = lane & 31;
+            o = *reinterpret_cast<const half8*>(t + (free0 + r) * BK + 8 * ((kc / 8 + (lane >> 5)) ^ ((r >> 2) & 3)));
         }
         return o;
     }
 
-    // Sums over nk steps into acc (which the caller has cleared or filled); ends with a barrier, after which the LDS
-    // is the caller's.
-    static __device__ inline void run(const Operand& a, const Operand& b, int nk, uint16_t* lds, floatx16 (&acc)[2][2])
+    // Sums over nk steps into acc (which the caller has cleared or filled).
+    static __device__ inline void run(const Operand& a, const Operand& b, int nk, uint16_t* lds, floatx16 (&acc)[TM][TN])
     {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wm = wave / 2, wn = wave % 2;
-        uint4 ra[TA][2], rb[TB][2];
-        int64_t oa[2], ob[2];
-        int pa[2], pb[2];
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds;
+        uint32_t oa[IA], ob[IB];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            oa[h] = source<TRA>(a.ld, tid + h * kBlock);
-            ob[h] = source<TRB>(b.ld, tid + h * kBlock);
-            pa[h] = place<TRA>(tid + h * kBlock);
-            pb[h] = place<TRB>(tid + h * kBlock);
-        }
-        auto load = [&](int step) {
-            const int64_t sa = (int64_t)step * (TRA ? BK * a.ld : BK), sb = (int64_t)step * (TRB ? BK * b.ld : BK);
+        for (int i = 0; i < IA; ++i) oa[i] = source<TRA, WA>(a.rows, wave * IA + i, lane);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+        for (int i = 0; i < IB; ++i) ob[i] = source<TRB, WB>(b.rows, wave * IB + i, lane);
+        const int64_t sa = TRA ? BK * BK : BK * a.rows, sb = TRB ? BK * BK : BK * b.rows;
+        auto load = [&](int step, int buffer) {
+            const uint32_t to = lds0 + (uint32_t)buffer * (BUFFER * 2);
 #pragma unroll
-                for (int t = 0; t < TA; ++t) ra[t][h] = *reinterpret_cast<const uint4*>(a.p + t * a.plane + sa + oa[h]);
+            for (int t = 0; t < TA; ++t)
 #pragma unroll
-                for (int t = 0; t < TB; ++t) rb[t][h] = *reinterpret_cast<const uint4*>(b.p + t * b.plane + sb + ob[h]);
-            }
-        };
-        auto put = [](uint16_t* p, const uint4& v) {
-            const uintx4 q = {v.x, v.y, v.z, v.w};
-            *(lds_uintx4*)p = q;
-        };
-        auto store = [&](uint16_t* buf) {
+                for (int i = 0; i < IA; ++i)
+                    load_to_lds(a.p + t * a.plane + step * sa, oa[i], to + (uint32_t)(t * PA * 2 + (wave * IA + i) * 1024));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int t = 0; t < TB; ++t)
 #pragma unroll
-                for (int t = 0; t < TA; ++t) put(buf + t * PLANE + pa[h], ra[t][h]);
-#pragma unroll
-                for (int t = 0; t < TB; ++t) put(buf + (TA + t) * PLANE + pb[h], rb[t][h]);
-            }
+                for (int i = 0; i < IB; ++i)
+                    load_to_lds(b.p + t * b.plane + step * sb, ob[i],
+                                to + (uint32_t)((TA * PA + t * PB) * 2 + (wave * IB + i) * 1024));
         };
         auto mma = [&](const uint16_t* buf) {
 #pragma unroll
             for (int kc = 0; kc < BK; kc += 16) {
-                half8 fa[TA][2], fb[TB][2];
+                half8 fa[TA][TM], fb[TB][TN];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
+                for (int t = 0; t < TA; ++t)
 #pragma unroll
-                    for (int t = 0; t < TA; ++t) fa[t][x] = fragment<TRA>(buf + t * PLANE, wm * 64 + x * 32, kc, lane);
+                    for (int x = 0; x < TM; ++x) fa[t][x] = fragment<TRA, WA>(buf + t * PA, (wm * TM + x) * 32, kc, lane);
 #pragma unroll
-                    for (int t = 0; t < TB; ++t)
-                        fb[t][x] = fragment<TRB>(buf + (TA + t) * PLANE, wn * 64 + x * 32, kc, lane);
-                }
+                for (int t = 0; t < TB; ++t)
+#pragma unroll
+                    for (int x = 0; x < TN; ++x)
+                        fb[t][x] = fragment<TRB, WB>(buf + TA * PA + t * PB, (wn * TN + x) * 32, kc, lane);
                 // the smaller products first
 #pragma unroll
-                for (int q = TA + TB - 2; q >= 0; --q)
+                for (int q = 1; q >= 0; --q)
 #pragma unroll
                     for (int t = 0; t < TA; ++t) {
                         const int u = q - t;
-                        if (u < 0 || u >= TB || t + u > 1) continue;
+                        if (u < 0 || u >= TB) continue;
 #pragma unroll
-                        for (int x = 0; x < 2; ++x)
+                        for (int x = 0; x < TM; ++x)
 #pragma unroll
-                            for (int y = 0; y < 2; ++y)
+                            for (int y = 0; y < TN; ++y)
                                 acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[t][x], fb[u][y], acc[x][y], 0, 0, 0);
                     }
             }
         };
-        if (nk > 0) {
-            load(0);
-            store(lds);
-            __syncthreads();
-            for (int i = 0; i < nk; ++i) {
-                if (i + 1 < nk) load(i + 1);
-                mma(lds + (i & 1) * BUFFER);
-                if (i + 1 < nk) store(lds + ((i + 1) & 1) * BUFFER);
-                __syncthreads();
-            }
+        clobber();
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < nk) load(s, s);
+        int cur = 0;  // buffer of the step
+        for (int i = 0; i < nk; ++i) {
+            // the steps after this one that are on their way may stay so, where all of them are
+            if (i + STAGES - 2 < nk) wait_and_meet<(STAGES - 2) * LOADS>();
+            else wait_and_meet<0>();
+            const int free = cur == 0 ? STAGES - 1 : cur - 1;
+            if (i + STAGES - 1 < nk) load(i + STAGES - 1, free);
+            mma(lds + cur * BUFFER);
+            cur = cur + 1 == STAGES ? 0 : cur + 1;
         }
     }
 };
 
-__device__ inline void clear(floatx16 (&acc)[2][2])
+template <int TM, int TN>
+__device__ inline void clear(floatx16 (&acc)[TM][TN])
 {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TM; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < TN; ++y)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
 }
@@ -439,47 +567,74 @@ __device__ inline int rows_here(const Meta* meta, uint32_t first, int piece_rows
 // ---- logits -------------------------------------------------------------------------------------
 // Tiles of logits come transposed, classes x rows, so that a lane holds classes of one row: sums over the classes stay
 // in the lane, but for one exchange of its halves.  In units of log 2: t = logit * log2(e).
+//
+// A workgroup takes 128 classes (a wavefront 64) and 64 TN rows.  Tiles are walked in groups of 8 tiles of classes: their
+// weights stay in the L2 of an XCD while the rows pass by.
+template <int TH, int TN>
+struct Logits {
+    using P = Product<2, TH, false, false, 2, TN, 2>;
+    static constexpr int ROWS = 64 * TN, GROUP = 8;
+    int c0, r0;  // first class and row of the tile
+
+    // false: no such tile.  The tiles of the rows there are, not of the grid, are dealt to the XCDs.
+    __device__ inline bool find(int live, int class_tiles)
+    {
+        const unsigned row_tiles = (unsigned)(live + ROWS - 1) / ROWS, tiles = row_tiles * (unsigned)class_tiles;
+        if (blockIdx.x >= tiles) return false;
+        const unsigned lid = xcd_local_index(blockIdx.x, tiles);
+        const unsigned group = lid / (GROUP * row_tiles), at = lid - group * (GROUP * row_tiles);
+        const unsigned width = (unsigned)class_tiles - group * GROUP < GROUP ? (unsigned)class_tiles - group * GROUP : GROUP;
+        r0 = __builtin_amdgcn_readfirstlane((int)(at / width) * ROWS);
+        c0 = __builtin_amdgcn_readfirstlane((int)(group * GROUP + at % width) * kTile);
+        return true;
+    }
+};
 
 // sums[piece of 64 classes][row] = { largest t, sum of 2^(t - largest) }; at_label[row] = t of the row's label.
-template <int TH>
-__global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* __restrict__ Wp, int kp, int cp, int c, int nk,
-                                                               const uint16_t* __restrict__ Hp, const int32_t* __restrict__ y,
+template <int TH, int TN>
+__global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
+                                                               const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
                                                                const Meta* __restrict__ meta, uint32_t first, int piece_rows,
                                                                int class_tiles, float2* __restrict__ sums,
                                                                float* __restrict__ at_label)
 {
-    using P = Product<2, TH, true, false>;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS];
-    const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int c0 = (int)(lid % class_tiles) * kTile, r0 = (int)(lid / class_tiles) * kTile;
-    if (r0 >= rows_here(meta, first, piece_rows)) return;
+    using L = Logits<TH, TN>;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[L::P::LDS];
+    L tile;
+    if (!tile.find(rows_here(meta, first, piece_rows), class_tiles)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-    floatx16 acc[2][2];
+    floatx16 acc[2][TN];
     clear(acc);
-    P::run({Wp + c0, cp, (size_t)kp * cp}, {Hp + (size_t)r0 * kp, kp, (size_t)piece_rows * kp}, nk, lds, acc);
+    L::P::run({Wp + (size_t)tile.c0 * BK, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds,
+              acc);
     const float a2 = meta->alpha * kLog2e;
-    const int cw = c0 + wm * 64;
-#pragma unroll
-    for (int yy = 0; yy < 2; ++yy) {
-        const int row = r0 + wn * 64 + yy * 32 + (lane & 31);
-        float t[2][16];
-        float top = -INFINITY;
+    const int cw = tile.c0 + wm * 64;
+    if (cw + kHalfTile > c)  // the last classes
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                t[x][v] = cw + x * 32 + tile_row(v, lane) < c ? acc[x][yy][v] * a2 : -INFINITY;
-                top = fmaxf(top, t[x][v]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float base = top == -INFINITY ? 0.f : top;
+            for (int v = 0; v < 16; ++v)
+                if (cw + x * 32 + tile_row(v, lane) >= c)
+#pragma unroll
+                    for (int yy = 0; yy < TN; ++yy) acc[x][yy][v] = -INFINITY;
+#pragma unroll
+    for (int yy = 0; yy < TN; ++yy) {
+        const int row = tile.r0 + (wn * TN + yy) * 32 + (lane & 31);
+        float most = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) most = fmaxf(most, acc[x][yy][v]);
+        most = fmaxf(most, __shfl_xor(most, 32, kWave));
+        const float top = most * a2;
+        const float base = most == -INFINITY ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(t[x][v] - base);
+            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -base));
         sum += __shfl_xor(sum, 32, kWave);
-        if (lane < 32) sums[(size_t)(cw / kHalfTile) * piece_rows + row] = make_float2(top, sum);
+        if (lane < 32) sums[(size_t)(cw / kHalfTile) * piece_rows + row] = make_float2(most == -INFINITY ? most : top, sum);
         const int at = y[row] - cw;
         if (__any(at >= 0 && at < kHalfTile)) {
             float mine = 0.f;
@@ -487,36 +642,47 @@ __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* _
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    if (at == x * 32 + tile_row(v, lane)) mine = t[x][v];
+                    if (at == x * 32 + tile_row(v, lane)) mine = acc[x][yy][v] * a2;
             if (at >= 0 && at < kHalfTile && ((at >> 2) & 1) == (lane >> 5)) at_label[row] = mine;
         }
     }
 }
 
 // A row's largest t and what its exponentials are taken times for G, from the sums of its pieces; the loss of the row.
+// A block takes ROWS rows, kBlock / ROWS lanes walk the pieces of each.
+template <int ROWS>
 __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restrict__ sums, int pieces,
                                                            const float* __restrict__ at_label,
                                                            const Meta* __restrict__ meta, uint32_t first, int piece_rows,
                                                            const uint32_t* __restrict__ rows, float2* __restrict__ norm,
                                                            float* __restrict__ losses, float* __restrict__ row_loss)
 {
-    // 16 rows per block, 16 lanes walk the pieces of each
-    __shared__ float tops[16][17], parts[16][17];
+    constexpr int LANES = kBlock / ROWS;
+    __shared__ float tops[LANES][ROWS + 1], parts[LANES][ROWS + 1];
     const int live = rows_here(meta, first, piece_rows);
-    const int j = threadIdx.x % 16, q = threadIdx.x / 16;
-    const int row = blockIdx.x * 16 + j;
-    if ((int)blockIdx.x * 16 >= live) return;
+    const int j = threadIdx.x % ROWS, q = threadIdx.x / ROWS;
+    const int row = blockIdx.x * ROWS + j;
+    if ((int)blockIdx.x * ROWS >= live) return;
     const int rr = row < live ? row : live - 1;
     float top = -INFINITY, sum = 0.f;
     bool bad = false;
-    for (int p = q; p < pieces; p += 16) {
-        const float2 s = sums[(size_t)p * piece_rows + rr];
-        bad = bad || !(s.y == s.y);
-        if (s.x > top) {
-            sum = sum * __builtin_amdgcn_exp2f(top - s.x) + s.y;
-            top = s.x;
-        } else if (s.x > -INFINITY) {
-            sum += s.y * __builtin_amdgcn_exp2f(s.x - top);
+    for (int p0 = q; p0 < pieces; p0 += 4 * LANES) {
+        float2 s[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int p = p0 + u * LANES;
+            s[u] = sums[(size_t)(p < pieces ? p : p0) * piece_rows + rr];
+            if (p >= pieces) s[u] = make_float2(-INFINITY, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            bad = bad || !(s[u].y == s[u].y);
+            if (s[u].x > top) {
+                sum = sum * __builtin_amdgcn_exp2f(top - s[u].x) + s[u].y;
+                top = s[u].x;
+            } else if (s[u].x > -INFINITY) {
+                sum += s[u].y * __builtin_amdgcn_exp2f(s[u].x - top);
+            }
         }
     }
     tops[q][j] = top;
@@ -524,16 +690,12 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
     __syncthreads();
     if (q == 0 && row < live) {
         float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, tops[i][j]);
+        for (int i = 0; i < LANES; ++i) m = fmaxf(m, tops[i][j]);
         float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s += parts[i][j] * (tops[i][j] > -INFINITY ? __builtin_amdgcn_exp2f(tops[i][j] - m) : 0.f);
-        // what is not a number stays one
+        // (what is not a number stays one: the lanes before it and after it add to it)
+        for (int i = 0; i < LANES; ++i)
+            s += parts[i][j] * (tops[i][j] > -INFINITY ? __builtin_amdgcn_exp2f(tops[i][j] - m) : 0.f);
         if (!(m > -INFINITY)) s = __uint_as_float(0x7FC00000u);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (!(parts[i][j] == parts[i][j])) s = parts[i][j];
         norm[row] = make_float2(m, kGradScale / s);
         const float l = ((m - at_label[row]) + log2f(s)) * kLn2;
         losses[first + row] = l;
@@ -545,117 +707,136 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
 __global__ __launch_bounds__(1024) void mean_loss_kernel(const float* __restrict__ losses, const Meta* __restrict__ meta,
                                                          double* __restrict__ loss)
 {
-    __shared__ double sh[1024];
-    const uint32_t count = meta->count;
+    __shared__ double sh[1024 / kWave];
+    const int64_t count = meta->count;
     double s = 0.0;
-    for (uint32_t i = threadIdx.x; i < count; i += 1024) s += (double)losses[i];
-    sh[threadIdx.x] = s;
-    __syncthreads();
-    for (int o = 512; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
-        __syncthreads();
+    for (int64_t i = threadIdx.x; i < count; i += 8 * 1024) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * 1024 < count ? losses[i + u * 1024] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += (double)v[u];
     }
-    if (threadIdx.x == 0) *loss = count ? sh[0] / (double)count : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.0;
+        for (int w = 0; w < 1024 / kWave; ++w) s += sh[w];
+        *loss = count ? s / (double)count : 0.0;
+    }
 }
 
 // ---- gradient with respect to the logits --------------------------------------------------------
-// planes[t][row][piece_cols]: 2^15 (softmax - onehot) of the classes [col0, col0 + piece_cols), zeros past the classes
+// planes[t], rows the listed ones and columns the classes from col0 on: 2^15 (softmax - onehot), zeros past the classes
 // and past the rows up to a whole tile.
-template <int TH>
-__global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* __restrict__ Wp, int kp, int cp, int c, int nk,
-                                                               const uint16_t* __restrict__ Hp, const int32_t* __restrict__ y,
+template <int TH, int TN>
+__global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
+                                                               const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
                                                                const float2* __restrict__ norm,
                                                                const Meta* __restrict__ meta, uint32_t first, int piece_rows,
-                                                               int col0, int piece_cols, int class_tiles,
+                                                               int col0, int g_rows, int class_tiles,
                                                                uint16_t* __restrict__ planes)
 {
-    using P = Product<2, TH, true, false>;
-    constexpr int PITCH = kTile + 8;  // 272 bytes
-    constexpr int NEED = kTile * PITCH > P::LDS ? kTile * PITCH : P::LDS;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[NEED];
-    const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int ct = (int)(lid % class_tiles) * kTile, r0 = (int)(lid / class_tiles) * kTile;
+    using L = Logits<TH, TN>;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[L::P::LDS];
     const int live = rows_here(meta, first, piece_rows);
-    if (r0 >= live) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
-    floatx16 acc[2][2];
+    L tile;
+    if (!tile.find(live, class_tiles)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+    floatx16 acc[2][TN];
     clear(acc);
-    P::run({Wp + col0 + ct, cp, (size_t)kp * cp}, {Hp + (size_t)r0 * kp, kp, (size_t)piece_rows * kp}, nk, lds, acc);
+    L::P::run({Wp + (size_t)(col0 + tile.c0) * BK, w_rows, (size_t)kp * w_rows},
+              {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds, acc);
     const float a2 = meta->alpha * kLog2e;
-    const int cw = col0 + ct + wm * 64;
-    uint2 lo[2][2][4];
+    const int cw = col0 + tile.c0 + wm * 64;
+    const bool edge = cw + kHalfTile > c;
+    const size_t plane = (size_t)class_tiles * kTile * g_rows;
 #pragma unroll
-    for (int yy = 0; yy < 2; ++yy) {
-        const int rt = wn * 64 + yy * 32 + (lane & 31), row = r0 + rt;
-        const bool in = row < live;
-        const float2 nm = in ? norm[row] : make_float2(0.f, 0.f);
-        const int at = in ? y[row] - cw : -1;
+    for (int yy = 0; yy < TN; ++yy) {
+        const int row = tile.r0 + (wn * TN + yy) * 32 + (lane & 31);
+        // rows past the last one have no features and so no logits: times zero they have no gradient
+        const float2 nm = row < live ? norm[row] : make_float2(0.f, 0.f);
+        const int at = y[row] - cw;
         const bool mark = __any(at >= 0 && at < kHalfTile);
+        uint16_t* const out = planes + ((size_t)((tile.c0 + wm * 64) / BK) * g_rows + row) * BK + 8 * (lane >> 5);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float g[4];
+            for (int q = 0; q < 4; q += 2) {
+                // two groups of 8 classes, of which this lane has the four at 4 (lane / 32)
+                uint32_t hi[2][2], lo[2][2];
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int i = x * 32 + tile_row(4 * q + b, lane);
-                    g[b] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][4 * q + b], a2, -nm.x)) * nm.y;
-                    if (mark && at == i) g[b] -= kGradScale;
-                    if (!in || cw + i >= c) g[b] = 0.f;
+                for (int u = 0; u < 2; ++u) {
+                    float g[4];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        g[b] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][4 * (q + u) + b], a2, -nm.x)) * nm.y;
+                    if (mark || edge)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            const int i = x * 32 + tile_row(4 * (q + u) + b, lane);
+                            if (at == i) g[b] -= kGradScale;
+                            if (cw + i >= c) g[b] = 0.f;
+                        }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        hi[u][b] = pack_f16(g[2 * b], g[2 * b + 1]);
+                        lo[u][b] = pack_f16(g[2 * b] - low_f16(hi[u][b]), g[2 * b + 1] - high_f16(hi[u][b]));
+                    }
                 }
-                const uint2 hi = make_uint2(pack_f16(g[0], g[1]), pack_f16(g[2], g[3]));
-                lo[x][yy][q] = make_uint2(pack_f16(g[0] - low_f16(hi.x), g[1] - high_f16(hi.x)),
-                                          pack_f16(g[2] - low_f16(hi.y), g[3] - high_f16(hi.y)));
-                *reinterpret_cast<uint2*>(lds + rt * PITCH + wm * 64 + x * 32 + 8 * q + 4 * (lane >> 5)) = hi;
+                // the halves of the wavefront exchange: each then has eight classes of a group in a row
+                auto put = [&](uint16_t* o, const uint32_t (&w)[2][2]) {
+                    const auto s0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+                    const auto s1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                    *reinterpret_cast<uint4*>(o + (size_t)x * g_rows * BK + 8 * q) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+                };
+                put(out, hi);
+                put(out + plane, lo);
             }
     }
-    auto flush = [&](uint16_t* out) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kTile * kTile / 8 / kBlock; ++i) {
-            const int p = tid + i * kBlock, r = p / 16, q = p % 16;
-            *reinterpret_cast<uint4*>(out + (size_t)(r0 + r) * piece_cols + ct + 8 * q) =
-                *reinterpret_cast<const uint4*>(lds + r * PITCH + 8 * q);
-        }
-        __syncthreads();
-    };
-    flush(planes);
-#pragma unroll
-    for (int yy = 0; yy < 2; ++yy)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint2*>(lds + (wn * 64 + yy * 32 + (lane & 31)) * PITCH + wm * 64 + x * 32 + 8 * q +
-                                          4 * (lane >> 5)) = lo[x][yy][q];
-    flush(planes + (size_t)piece_rows * piece_cols);
 }
 
 // ---- dH -----------------------------------------------------------------------------------------
-// part[slab][row][kp] (+)= G[row][classes of the slab] W'^T
+// part[slab][row][kp] (+)= G[row][classes of the slab] W'^T.  One term each (bf16 features, whose gradient is rounded
+// to 8 bits afterwards) or two.
 template <int T>
-__global__ __launch_bounds__(kBlock, 2) void grad_rows_kernel(const uint16_t* __restrict__ Gp, int piece_cols, int piece_rows,
-                                                              const uint16_t* __restrict__ Wp, int kp, int cp, int col0,
+struct GradRows {
+    static constexpr int TM = T == 1 ? 4 : 2, TN = 2, STAGES = T == 1 ? 3 : 2;
+    using P = Product<T, T, false, true, TM, TN, STAGES>;
+    static constexpr int ROWS = 64 * TM;
+};
+
+template <int T>
+__global__ __launch_bounds__(kBlock, 2) void grad_rows_kernel(const uint16_t* __restrict__ Gp, int g_rows, int piece_cols,
+                                                              int piece_rows, const uint16_t* __restrict__ Wp, int kp,
+                                                              int w_rows, int col0,
                                                               const Meta* __restrict__ meta, uint32_t first, int slab_cols,
                                                               int k_tiles, int slabs, bool add, float* __restrict__ part)
 {
-    using P = Product<T, T, false, false>;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS];
-    const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int kt = (int)(lid % k_tiles), slab = (int)(lid / k_tiles) % slabs, r0 = (int)(lid / (k_tiles * slabs)) * kTile;
-    if (r0 >= rows_here(meta, first, piece_rows)) return;
+    using S = GradRows<T>;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[S::P::LDS];
+    const unsigned row_tiles = (unsigned)(rows_here(meta, first, piece_rows) + S::ROWS - 1) / S::ROWS;
+    const unsigned tiles = row_tiles * (unsigned)(k_tiles * slabs);
+    if (blockIdx.x >= tiles) return;
+    const unsigned lid = xcd_local_index(blockIdx.x, tiles);
+    const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
+    const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % slabs));
+    const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * slabs)) * S::ROWS);
     const int s0 = slab * slab_cols;
     const int s1 = s0 + slab_cols < piece_cols ? s0 + slab_cols : piece_cols;
+    if (add && s1 <= s0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-    float* const out = part + ((size_t)slab * piece_rows + r0 + wm * 64) * kp + kt * kTile + wn * 64 + (lane & 31);
-    floatx16 acc[2][2];
+    floatx16 acc[S::TM][S::TN];
     clear(acc);
-    P::run({Gp + (size_t)r0 * piece_cols + s0, piece_cols, (size_t)piece_rows * piece_cols},
-           {Wp + (size_t)kt * kTile * cp + col0 + s0, cp, (size_t)kp * cp}, s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
+    S::P::run({Gp + ((size_t)(s0 / BK) * g_rows + r0) * BK, g_rows, (size_t)piece_cols * g_rows},
+              {Wp + ((size_t)(kt * kTile / BK) * w_rows + col0 + s0) * BK, w_rows, (size_t)kp * w_rows}, s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
+    float* const out = part + ((size_t)slab * piece_rows + r0 + wm * S::TM * 32) * kp + kt * kTile + wn * 64 + (lane & 31);
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < S::TM; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < S::TN; ++y)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 float* const o = out + (size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32;
@@ -663,99 +844,102 @@ __global__ __launch_bounds__(kBlock, 2) void grad_rows_kernel(const uint16_t* __
             }
 }
 
+// The sum of four neighboring cells over the slabs, for SL lanes that share the cells: lane 0 of them has it.
+template <int SL>
+__device__ inline float4 sum_slabs(const float* p, size_t slab, int slabs, bool in, float4 (*lds)[kBlock / SL])
+{
+    const int item = threadIdx.x % (kBlock / SL), l = threadIdx.x / (kBlock / SL);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int b = l; in && b < slabs; b += 4 * SL) {
+        float4 t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            t[u] = b + u * SL < slabs ? *reinterpret_cast<const float4*>(p + (b + u * SL) * slab) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            s.x += t[u].x;
+            s.y += t[u].y;
+            s.z += t[u].z;
+            s.w += t[u].w;
+        }
+    }
+    if (SL == 1) return s;
+    lds[l][item] = s;
+    __syncthreads();
+    if (l == 0)
+#pragma unroll
+        for (int i = 1; i < SL; ++i) {
+            const float4 t = lds[i][item];
+            s.x += t.x;
+            s.y += t.y;
+            s.z += t.z;
+            s.w += t.w;
+        }
+    return s;
+}
+
 // dH of the listed rows from the slabs' sums.
-template <bool BF16>
+template <bool BF16, int SL>
 __global__ __launch_bounds__(kBlock) void finish_rows_kernel(const float* __restrict__ part, int slabs, int piece_rows, int k,
                                                              int kp, const int32_t* __restrict__ shift,
                                                              const Meta* __restrict__ meta, uint32_t first,
                                                              const uint32_t* __restrict__ rows, void* __restrict__ dH,
                                                              int64_t ldd)
 {
+    __shared__ float4 lds[SL][kBlock / SL];
     const int live = rows_here(meta, first, piece_rows);
-    const float inv = 1.f / (float)meta->count;
     const int per_row = (k + 3) / 4;
-    const int64_t items = (int64_t)live * per_row;
-    const size_t slab = (size_t)piece_rows * kp;
-    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)gridDim.x * kBlock) {
-        const int i = (int)(it / per_row), j = (int)(it % per_row) * 4;
-        const float* const p = part + (size_t)i * kp + j;
-        float4 s = *reinterpret_cast<const float4*>(p);
-        for (int b = 1; b < slabs; ++b) {
-            const float4 t = *reinterpret_cast<const float4*>(p + b * slab);
-            s.x += t.x;
-            s.y += t.y;
-            s.z += t.z;
-            s.w += t.w;
-        }
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        float o[4];
+    const int64_t it = (int64_t)blockIdx.x * (kBlock / SL) + threadIdx.x % (kBlock / SL);
+    if ((int64_t)blockIdx.x * (kBlock / SL) >= (int64_t)live * per_row) return;
+    const bool in = it < (int64_t)live * per_row;
+    const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
+    const float4 s = sum_slabs<SL>(part + (size_t)i * kp + j, (size_t)piece_rows * kp, slabs, in, lds);
+    if (!in || threadIdx.x >= kBlock / SL) return;
+    const float inv = 1.f / (float)meta->count;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    float o[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - shift[kp + j + b]);
-        const int64_t at = (int64_t)rows[first + i] * ldd + j;
-        if (BF16) {
-            const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-            if (j + 4 <= k) *reinterpret_cast<uint2*>((uint16_t*)dH + at) = make_uint2(w[0], w[1]);
-            else
-                for (int b = 0; j + b < k; ++b) ((uint16_t*)dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
-        } else {
-            if (j + 4 <= k) *reinterpret_cast<float4*>((float*)dH + at) = make_float4(o[0], o[1], o[2], o[3]);
-            else
-                for (int b = 0; j + b < k; ++b) ((float*)dH)[at + b] = o[b];
-        }
-    }
-}
-
-// Zeros for the rows without a label: of dH (cols > 0) and of the losses of the rows.
-template <bool BF16>
-__global__ __launch_bounds__(kBlock) void clear_rows_kernel(const int32_t* __restrict__ labels, int64_t n, int32_t c,
-                                                            void* __restrict__ dH, int64_t ldd, int k,
-                                                            float* __restrict__ row_loss)
-{
-    const int per_row = (k + 3) / 4 + (k == 0);
-    const int64_t items = n * per_row;
-    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)gridDim.x * kBlock) {
-        const int64_t r = it / per_row;
-        const int j = (int)(it - r * per_row) * 4;
-        if (has_label(labels[r], c)) continue;
-        if (j == 0 && row_loss) row_loss[r] = 0.f;
-        const int64_t at = r * ldd + j;
-        if (j + 4 <= k) {
-            if (BF16) *reinterpret_cast<uint2*>((uint16_t*)dH + at) = make_uint2(0u, 0u);
-            else *reinterpret_cast<float4*>((float*)dH + at) = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-            for (int b = 0; j + b < k; ++b) {
-                if (BF16) ((uint16_t*)dH)[at + b] = 0;
-                else ((float*)dH)[at + b] = 0.f;
-            }
-        }
+    for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - shift[kp + j + b]);
+    const int64_t at = (int64_t)rows[first + i] * ldd + j;
+    if (BF16) {
+        const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+        if (j + 4 <= k) *reinterpret_cast<uint2*>((uint16_t*)dH + at) = make_uint2(w[0], w[1]);
+        else
+            for (int b = 0; j + b < k; ++b) ((uint16_t*)dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
+    } else {
+        if (j + 4 <= k) *reinterpret_cast<float4*>((float*)dH + at) = make_float4(o[0], o[1], o[2], o[3]);
+        else
+            for (int b = 0; j + b < k; ++b) ((float*)dH)[at + b] = o[b];
     }
 }
 
 // ---- dW -----------------------------------------------------------------------------------------
-// part[slab][kp][piece_cols] = H'^T[rows of the slab] G
-template <int TH>
-__global__ __launch_bounds__(kBlock, 2) void grad_weights_kernel(const uint16_t* __restrict__ Hp, int kp,
-                                                                 const uint16_t* __restrict__ Gp, int piece_cols,
+// part[slab][kp][piece_cols] = H'^T[rows of the slab] G.  Tiles of 64 TM features x 128 classes.
+template <int TH, int TM>
+__global__ __launch_bounds__(kBlock, 2) void grad_weights_kernel(const uint16_t* __restrict__ Hp, int kp, int h_rows,
+                                                                 const uint16_t* __restrict__ Gp, int g_rows, int piece_cols,
                                                                  int piece_rows, const Meta* __restrict__ meta, uint32_t first,
                                                                  int class_tiles, int k_tiles, int slabs,
                                                                  float* __restrict__ part)
 {
-    using P = Product<TH, 2, true, true>;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS];
+    using P = Product<TH, 2, true, true, TM, 2, 2>;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[P::LDS];
     const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int kt = (int)(lid % k_tiles), ct = (int)(lid / k_tiles) % class_tiles, slab = (int)(lid / (k_tiles * class_tiles));
+    const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
+    const int ct = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % class_tiles));
+    const int slab = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * class_tiles)));
     const int live = rows_here(meta, first, piece_rows);
     const int per = ((live + slabs - 1) / slabs + BK - 1) / BK * BK;
     const int r0 = slab * per, r1 = r0 + per < live ? r0 + per : live;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-    floatx16 acc[2][2];
+    floatx16 acc[TM][2];
     clear(acc);
-    P::run({Hp + (size_t)r0 * kp + kt * kTile, kp, (size_t)piece_rows * kp},
-           {Gp + (size_t)r0 * piece_cols + ct * kTile, piece_cols, (size_t)piece_rows * piece_cols},
+    P::run({Hp + ((size_t)(kt * P::WA / BK) * h_rows + r0) * BK, h_rows, (size_t)kp * h_rows},
+           {Gp + ((size_t)(ct * kTile / BK) * g_rows + r0) * BK, g_rows, (size_t)piece_cols * g_rows},
            r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
-    float* const out = part + ((size_t)slab * kp + kt * kTile + wm * 64) * piece_cols + ct * kTile + wn * 64 + (lane & 31);
+    float* const out = part + ((size_t)slab * kp + kt * P::WA + wm * TM * 32) * piece_cols + ct * kTile + wn * 64 + (lane & 31);
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TM; ++x)
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -764,32 +948,34 @@ __global__ __launch_bounds__(kBlock, 2) void grad_weights_kernel(const uint16_t*
 }
 
 // dW[k][classes of the piece] (+)= the slabs' sums, unscaled.
+template <int SL>
 __global__ __launch_bounds__(kBlock) void finish_weights_kernel(const float* __restrict__ part, int slabs, int k, int kp,
                                                                 int piece_cols, int cols, const int32_t* __restrict__ shift,
                                                                 const Meta* __restrict__ meta, uint32_t first, bool add,
                                                                 float* __restrict__ dW, int64_t ldw)
 {
+    __shared__ float4 lds[SL][kBlock / SL];
     const uint32_t count = meta->count;
     if (add && first >= count) return;
-    const float inv = count ? 1.f / (float)count : 0.f;
     const int per_row = (cols + 3) / 4;
-    const int64_t items = (int64_t)k * per_row;
-    const size_t slab = (size_t)kp * piece_cols;
-    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)gridDim.x * kBlock) {
-        const int i = (int)(it / per_row), j = (int)(it % per_row) * 4;
-        const float* const p = part + (size_t)i * piece_cols + j;
-        float4 s = *reinterpret_cast<const float4*>(p);
-        for (int b = 1; b < slabs; ++b) {
-            const float4 t = *reinterpret_cast<const float4*>(p + b * slab);
-            s.x += t.x;
-            s.y += t.y;
-            s.z += t.z;
-            s.w += t.w;
+    const int64_t it = (int64_t)blockIdx.x * (kBlock / SL) + threadIdx.x % (kBlock / SL);
+    const bool in = it < (int64_t)k * per_row;
+    const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
+    const float4 s = sum_slabs<SL>(part + (size_t)i * piece_cols + j, (size_t)kp * piece_cols, slabs, in, lds);
+    if (!in || threadIdx.x >= kBlock / SL) return;
+    const float inv = count ? 1.f / (float)count : 0.f;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    float* const o = dW + (int64_t)i * ldw + j;
+    const int e = -15 - shift[i];
+    if (j + 4 <= cols) {
+        float4 g = make_float4(ldexpf(v[0] * inv, e), ldexpf(v[1] * inv, e), ldexpf(v[2] * inv, e), ldexpf(v[3] * inv, e));
+        if (add) {
+            const float4 d = *reinterpret_cast<const float4*>(o);
+            g = make_float4(d.x + g.x, d.y + g.y, d.z + g.z, d.w + g.w);
         }
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        float* const o = dW + (int64_t)i * ldw + j;
-        const int e = -15 - shift[i];
-        for (int b = 0; b < 4 && j + b < cols; ++b) {
+        *reinterpret_cast<float4*>(o) = g;
+    } else {
+        for (int b = 0; j + b < cols; ++b) {
             const float g = ldexpf(v[b] * inv, e);
             o[b] = add ? o[b] + g : g;
         }
@@ -800,47 +986,49 @@ __global__ __launch_bounds__(kBlock) void finish_weights_kernel(const float* __r
 
 struct Layout {
     int kp, cp, terms;              // padded widths; terms of a feature
+    int h_rows, w_rows, g_rows;     // rows of a block of 32 columns of the features, the weights and G
     int piece_rows, piece_cols;     // a block of G
     int row_pieces, col_pieces;
     int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
-    int w_slabs;                    // dW: rows of a piece dealt to slabs
-    int64_t list_blocks;
+    int w_slabs, w_width;           // dW: rows of a piece dealt to slabs; features of a tile
+    int list_step, list_blocks;
     size_t meta, counts, rows, top, shift, hp, wp, y, sums, at_label, norm, losses, g, dh, dw, bytes;
 };
 
-int up(int64_t x, int to) { return (int)(ceil_div(x, to) * to); }
+int64_t up(int64_t x, int64_t to) { return ceil_div(x, to) * to; }
+int64_t between(int64_t lo, int64_t x, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
 {
     Layout l;
     l.terms = dtype == MIXGCN_BF16 ? 1 : 2;
-    l.kp = up(k, kTile);
-    l.cp = up(c, kTile);
-    // G of a block of rows and classes takes at most 128 MB, which the last-level cache holds
-    const int64_t most = ((int64_t)128 << 20) / 4;
-    const int64_t all_rows = n > 0 ? up(n < (1 << 30) ? n : (1 << 30), kTile) : kTile;
-    int64_t rows = most / l.cp / kTile * kTile;
-    if (rows < 16384) rows = 16384;
-    if (rows > all_rows) rows = all_rows;
-    if (rows > 131072) rows = 131072;
-    l.piece_rows = (int)rows;
-    int64_t cols = most / rows / kTile * kTile;
+    l.kp = (int)up(k, kTile);
+    l.cp = (int)up(c, kTile);
+    // G, four bytes a logit, is handed on in blocks of 2^26 logits at most: as many classes as give dW a tile for
+    // every compute unit without a split of the rows, and rows for the rest
+    const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
+    int64_t cols = between(2048, up(32768 / (l.kp / kTile), kTile), 32768);
     if (cols > l.cp) cols = l.cp;
+    int64_t rows = between(2048, most / cols / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
+    if (rows > all_rows) rows = all_rows;
+    cols = between(kTile, most / rows / kTile * kTile, l.cp);
+    l.piece_rows = (int)rows;
     l.piece_cols = (int)cols;
+    // (two more: blocks a power of two apart would begin in the same channel of the L2)
+    l.h_rows = l.g_rows = (int)rows + 2;
+    l.w_rows = l.cp + 2;
     l.row_pieces = (int)ceil_div(all_rows, rows);
     l.col_pieces = (int)ceil_div(l.cp, cols);
-    const int64_t k_tiles = l.kp / kTile, row_tiles = rows / kTile, col_tiles = cols / kTile;
-    // enough workgroups for every compute unit
-    int64_t s = 512 / (k_tiles * row_tiles);
-    if (s > col_tiles) s = col_tiles;
-    if (s < 1) s = 1;
+    const int64_t k_tiles = l.kp / kTile, col_tiles = cols / kTile;
+    // two workgroups for every compute unit
+    const int64_t row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1>::ROWS : GradRows<2>::ROWS);
+    int64_t s = between(1, 512 / (k_tiles * row_tiles), col_tiles);
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
-    s = 512 / (k_tiles * col_tiles);
-    if (s > row_tiles) s = row_tiles;
-    if (s < 1) s = 1;
-    l.w_slabs = (int)s;
-    l.list_blocks = ceil_div(n, kListRows);
+    l.w_width = l.terms == 1 && l.kp % 256 == 0 ? 256 : 128;
+    l.w_slabs = (int)between(1, 512 / (l.kp / l.w_width * col_tiles), rows / kTile);
+    l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
+    l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
@@ -852,8 +1040,8 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.rows = take((size_t)n * 4);
     l.top = take((size_t)l.kp * 8);
     l.shift = take((size_t)l.kp * 8);
-    l.hp = take((size_t)l.terms * rows * l.kp * 2);
-    l.wp = take((size_t)2 * l.kp * l.cp * 2);
+    l.hp = take((size_t)l.terms * l.h_rows * l.kp * 2);
+    l.wp = take((size_t)2 * l.kp * l.w_rows * 2);
     l.y = take((size_t)rows * 4);
     l.sums = take((size_t)(l.cp / kHalfTile) * rows * 8);
     l.at_label = take((size_t)rows * 4);
@@ -861,7 +1049,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.losses = take((size_t)n * 4);
     l.g = l.dh = l.dw = 0;
     if (gradients) {
-        l.g = take((size_t)2 * rows * cols * 2);
+        l.g = take((size_t)2 * l.g_rows * cols * 2);
         l.dh = take((size_t)l.row_slabs * rows * l.kp * 4);
         l.dw = take((size_t)l.w_slabs * l.kp * cols * 4);
     }
@@ -869,11 +1057,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     return l;
 }
 
-unsigned grid_for(int64_t items)
-{
-    const int64_t g = ceil_div(items, kBlock);
-    return (unsigned)(g < 1 ? 1 : g > 8192 ? 8192 : g);
-}
+unsigned grid_for(int64_t items) { return (unsigned)between(1, ceil_div(items, kBlock), 8192); }
 
 }  // namespace
 
@@ -904,54 +1088,96 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     uint16_t* const g = (uint16_t*)(ws + l.g);
     float* const dhp = (float*)(ws + l.dh);
     float* const dwp = (float*)(ws + l.dw);
-#define MIXGCN_RUN(KERNEL, GRID, ...) hipLaunchKernelGGL(KERNEL, dim3((unsigned)(GRID)), dim3(kBlock), 0, s, __VA_ARGS__)
-#define MIXGCN_RUN_T(KERNEL, YES, NO, GRID, ...)              \
-    do {                                                      \
-        if (bf16) MIXGCN_RUN(KERNEL<YES>, GRID, __VA_ARGS__); \
-        else MIXGCN_RUN(KERNEL<NO>, GRID, __VA_ARGS__);       \
+#define MIXGCN_RUN(KERNEL, GRID, ...) hipLaunchKernelGGL((KERNEL), dim3((unsigned)(GRID)), dim3(kBlock), 0, s, __VA_ARGS__)
+#define MIXGCN_RUN_T(KERNEL, GRID, ...)                         \
+    do {                                                        \
+        if (bf16) MIXGCN_RUN(KERNEL<true>, GRID, __VA_ARGS__);  \
+        else MIXGCN_RUN(KERNEL<false>, GRID, __VA_ARGS__);      \
     } while (0)
-    const unsigned list_grid = (unsigned)(l.list_blocks > 0 ? l.list_blocks : 1);
-    if (list_grid > 1) MIXGCN_RUN(count_labels_kernel, list_grid, labels, n, c, counts);
-    MIXGCN_RUN(list_labels_kernel, list_grid, labels, n, c, counts, rows, meta, top, 2 * l.kp);
-    const int w_pieces = (int)ceil_div(c, kMaxCols), w_blocks = w_pieces * k;
-    const int h_rows = n > 65536 ? (int)ceil_div(n, 1024) : 64;
-    MIXGCN_RUN_T(top_kernel, true, false, w_blocks + ceil_div(n, h_rows), H, ldh, rows, meta, W, ldw, k, c, l.kp, w_blocks,
-                 w_pieces, h_rows, top);
-    MIXGCN_RUN(scale_kernel, 1, top, k, l.kp, shift, meta);
-    MIXGCN_RUN(split_weights_kernel, grid_for((int64_t)l.kp * l.cp / 8), W, ldw, k, c, l.kp, l.cp, shift, wp);
-    if (row_loss || dH) MIXGCN_RUN_T(clear_rows_kernel, true, false, grid_for(n * (dH ? (k + 3) / 4 : 1)), labels, n, c, dH, ldd,
-                                     dH ? k : 0, row_loss);
-    const int nk = (int)ceil_div(k, BK), k_tiles = l.kp / kTile, class_tiles = l.cp / kTile, row_tiles = l.piece_rows / kTile;
+    if (l.list_blocks > 1) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts);
+    MIXGCN_RUN(list_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, rows, meta, top, 2 * l.kp);
+    TopPlan tp;
+    tp.w_pieces = (int)ceil_div(c, kTopCols);
+    tp.w_blocks = tp.w_pieces * k;
+    tp.h_rows = (int)between(64, ceil_div(n, 1024), (int64_t)1 << 30);
+    tp.h_blocks = (int)ceil_div(n, tp.h_rows);
+    tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), kBlock), 4096) : 0;
+    MIXGCN_RUN_T(top_kernel, tp.w_blocks + tp.h_blocks + tp.clear_blocks, H, ldh, rows, meta, W, ldw, k, c, l.kp, tp, top, labels,
+                 n, dH, ldd, row_loss);
+    const int nk = (int)ceil_div(k, BK), k_tiles = l.kp / kTile, class_tiles = l.cp / kTile, pr = l.piece_rows;
+    const int pieces = l.cp / kHalfTile;
+    // rows of a tile of logits: few of them for few rows, as many as the registers hold for bf16 features, whose one
+    // plane is read from LDS for two planes of weights
+    const int logit_rows = pr <= 256 && n <= 64 ? 64 : bf16 ? 256 : 128;
+#define MIXGCN_LOGITS(KERNEL, CLASS_TILES, ...)                                                         \
+    do {                                                                                                \
+        const int64_t grid = (int64_t)(CLASS_TILES) * (pr / logit_rows);                                \
+        if (bf16 && logit_rows == 64) MIXGCN_RUN((KERNEL<1, 1>), grid, __VA_ARGS__);                    \
+        else if (bf16) MIXGCN_RUN((KERNEL<1, 4>), grid, __VA_ARGS__);                                   \
+        else if (logit_rows == 64) MIXGCN_RUN((KERNEL<2, 1>), grid, __VA_ARGS__);                       \
+        else MIXGCN_RUN((KERNEL<2, 2>), grid, __VA_ARGS__);                                             \
+    } while (0)
     for (int rp = 0; rp < l.row_pieces; ++rp) {
-        const uint32_t first = (uint32_t)rp * (uint32_t)l.piece_rows;
-        const int pr = l.piece_rows;
-        MIXGCN_RUN_T(split_rows_kernel, true, false, grid_for((int64_t)pr * l.kp / 8), H, ldh, rows, labels, meta, first, pr, k,
-                     l.kp, shift, hp, y);
-        MIXGCN_RUN_T(logit_sums_kernel, 1, 2, (int64_t)class_tiles * row_tiles, wp, l.kp, l.cp, c, nk, hp, y, meta, first, pr,
-                     class_tiles, sums, at_label);
-        MIXGCN_RUN(join_sums_kernel, ceil_div(pr, 16), sums, l.cp / kHalfTile, at_label, meta, first, pr, rows, norm, losses,
-                   row_loss);
+        const uint32_t first = (uint32_t)rp * (uint32_t)pr;
+        const int w_blocks = rp == 0 ? (int)grid_for((int64_t)l.kp / BK * l.cp) : 0;
+        MIXGCN_RUN_T(split_kernel, w_blocks + grid_for((int64_t)pr * l.kp / 8), H, ldh, rows, labels, meta, first, pr, l.h_rows, k,
+                     l.kp, top, shift, hp, y, w_blocks, W, ldw, c, l.cp, l.w_rows, wp);
+        MIXGCN_LOGITS(logit_sums_kernel, class_tiles, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, class_tiles, sums, at_label);
+        // few rows: more lanes to each
+        if (pr <= 4096)
+            MIXGCN_RUN(join_sums_kernel<4>, pr / 4, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
+        else
+            MIXGCN_RUN(join_sums_kernel<16>, pr / 16, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
         for (int q = 0; grads && q < l.col_pieces; ++q) {
             const int col0 = q * l.piece_cols;
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
             const int cols = c - col0 < pc ? c - col0 : pc;
-            MIXGCN_RUN_T(logit_grad_kernel, 1, 2, (int64_t)ct * row_tiles, wp, l.kp, l.cp, c, nk, hp, y, norm, meta, first, pr, col0,
-                         pc, ct, g);
-            if (dH)
-                MIXGCN_RUN_T(grad_rows_kernel, 1, 2, (int64_t)k_tiles * l.row_slabs * row_tiles, g, pc, pr, wp, l.kp, l.cp, col0,
-                             meta, first, l.row_slab_cols, k_tiles, l.row_slabs, q > 0, dhp);
+            MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
+            if (dH) {
+                const int64_t tiles = (int64_t)k_tiles * l.row_slabs;
+                if (bf16)
+                    MIXGCN_RUN(grad_rows_kernel<1>, tiles * ceil_div(pr, GradRows<1>::ROWS), g, l.g_rows, pc, pr, wp, l.kp, l.w_rows, col0, meta,
+                               first, l.row_slab_cols, k_tiles, l.row_slabs, q > 0, dhp);
+                else
+                    MIXGCN_RUN(grad_rows_kernel<2>, tiles * ceil_div(pr, GradRows<2>::ROWS), g, l.g_rows, pc, pr, wp, l.kp, l.w_rows, col0, meta,
+                               first, l.row_slab_cols, k_tiles, l.row_slabs, q > 0, dhp);
+            }
             if (dW) {
-                MIXGCN_RUN_T(grad_weights_kernel, 1, 2, (int64_t)k_tiles * ct * l.w_slabs, hp, l.kp, g, pc, pr, meta, first, ct,
-                             k_tiles, l.w_slabs, dwp);
-                MIXGCN_RUN(finish_weights_kernel, grid_for((int64_t)k * ceil_div(cols, 4)), dwp, l.w_slabs, k, l.kp, pc, cols,
-                           shift, meta, first, rp > 0, dW + col0, ldg);
+                const int wt = l.kp / l.w_width;
+                const int64_t grid = (int64_t)wt * ct * l.w_slabs;
+                if (bf16 && l.w_width == 256)
+                    MIXGCN_RUN((grad_weights_kernel<1, 4>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
+                else if (bf16)
+                    MIXGCN_RUN((grad_weights_kernel<1, 2>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
+                else
+                    MIXGCN_RUN((grad_weights_kernel<2, 2>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
+                const int64_t items = (int64_t)k * ceil_div(cols, 4);
+                if (l.w_slabs > 4)
+                    MIXGCN_RUN(finish_weights_kernel<16>, ceil_div(items, kBlock / 16), dwp, l.w_slabs, k, l.kp, pc, cols, shift, meta,
+                               first, rp > 0, dW + col0, ldg);
+                else
+                    MIXGCN_RUN(finish_weights_kernel<1>, ceil_div(items, kBlock), dwp, l.w_slabs, k, l.kp, pc, cols, shift, meta,
+                               first, rp > 0, dW + col0, ldg);
             }
         }
-        if (dH)
-            MIXGCN_RUN_T(finish_rows_kernel, true, false, grid_for((int64_t)pr * ceil_div(k, 4)), dhp, l.row_slabs, pr, k, l.kp,
-                         shift, meta, first, rows, dH, ldd);
+        if (dH) {
+            const int64_t items = (int64_t)pr * ceil_div(k, 4);
+#define MIXGCN_FINISH(SL)                                                                                                   \
+    do {                                                                                                                    \
+        if (bf16)                                                                                                           \
+            MIXGCN_RUN((finish_rows_kernel<true, SL>), ceil_div(items, kBlock / SL), dhp, l.row_slabs, pr, k, l.kp, shift, meta, \
+                       first, rows, dH, ldd);                                                                               \
+        else                                                                                                                \
+            MIXGCN_RUN((finish_rows_kernel<false, SL>), ceil_div(items, kBlock / SL), dhp, l.row_slabs, pr, k, l.kp, shift, meta, \
+                       first, rows, dH, ldd);                                                                               \
+    } while (0)
+            if (l.row_slabs > 4) MIXGCN_FINISH(16);
+            else MIXGCN_FINISH(1);
+#undef MIXGCN_FINISH
+        }
     }
     if (loss) hipLaunchKernelGGL(mean_loss_kernel, dim3(1), dim3(1024), 0, s, losses, meta, loss);
+#undef MIXGCN_LOGITS
 #undef MIXGCN_RUN_T
 #undef MIXGCN_RUN
     MIXGCN_HIP_TRY(hipGetLastError());

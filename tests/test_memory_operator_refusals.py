@@ -41,7 +41,7 @@ def test_linear_xent_refuses(lib, change, word):
     assert word in lib.mixgcn_last_error(), lib.mixgcn_last_error()
 
 
-@pytest.mark.parametrize("change", [dict(n=(1 << 30) + 1), dict(k=(1 << 16) + 4, ldh=1 << 17), dict(c=(1 << 24) + 4, ldw=1 << 25)])
+@pytest.mark.parametrize("change", [dict(n=(1 << 30) + 1), dict(k=(1 << 16) + 4, ldh=1 << 17), dict(c=(1 << 22) + 4, ldw=1 << 25)])
 def test_linear_xent_beyond_its_sizes(lib, change):
     assert xent(lib, **change) == -5
 
@@ -49,7 +49,7 @@ def test_linear_xent_beyond_its_sizes(lib, change):
 def test_linear_xent_workspace_sizes(lib):
     f = lib.mixgcn_linear_xent_workspace
     for bad in ((2, 1, 1, 1, 0), (0, -1, 1, 1, 0), (0, 1, 0, 1, 0), (0, 1, 1, 0, 0), (0, (1 << 30) + 1, 1, 1, 0),
-                (0, 1, (1 << 16) + 1, 1, 0), (0, 1, 1, (1 << 24) + 1, 0)):
+                (0, 1, (1 << 16) + 1, 1, 0), (0, 1, 1, (1 << 22) + 1, 0)):
         assert f(*bad) == -1
     assert 0 < f(0, 0, 1, 1, 0) <= f(0, 0, 1, 1, 1)
     assert f(0, 1000, 64, 500, 0) < f(0, 1000, 64, 500, 1)
@@ -59,7 +59,7 @@ def test_linear_xent_workspace_sizes(lib):
         assert f(dtype, n, k, c, 1) < 0.03 * 2 * n * c * es * (2 if es == 2 else 1)
         assert f(dtype, 1 << 30, 64, 1000, 1) - 8 * (1 << 30) < 1 << 31
     # the largest sizes do not overflow
-    assert f(0, 1 << 30, 1 << 16, 1 << 24, 1) > 1 << 40
+    assert f(0, 1 << 30, 1 << 16, 1 << 22, 1) > 1 << 40
 
 
 def checkpoint(lib, what, **change):
