@@ -222,7 +222,13 @@ __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H,
             const uint32_t t = __shfl_xor(m, o, kWave);
             m = t > m ? t : m;
         }
-        if ((tid & 63) == 0) atomicMax(top + kp + row, m);
+        if ((tid & 63) == 0) col_top[tid >> 6] = m;
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int i = 1; i < kBlock / kWave; ++i) m = col_top[i] > m ? col_top[i] : m;
+            atomicMax(top + kp + row, m);
+        }
     } else if (b < plan.w_blocks + plan.h_blocks) {
         const uint32_t count = meta->count, i0 = (uint32_t)(b - plan.w_blocks) * (uint32_t)plan.h_rows;
         const int m_rows = i0 >= count ? 0 : count - i0 < (uint32_t)plan.h_rows ? (int)(count - i0) : plan.h_rows;
@@ -834,14 +840,24 @@ __global__ __launch_bounds__(kBlock, 2) void grad_rows_kernel(const uint16_t* __
               {Wp + ((size_t)(kt * kTile / BK) * w_rows + col0 + s0) * BK, w_rows, (size_t)kp * w_rows}, s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
     float* const out = part + ((size_t)slab * piece_rows + r0 + wm * S::TM * 32) * kp + kt * kTile + wn * 64 + (lane & 31);
 #pragma unroll
-    for (int x = 0; x < S::TM; ++x)
+    for (int x = 0; x < S::TM; ++x) {
+        if (add) {
+            // all loads of a row of tiles before its first store (left to follow each other they cost 56 us a piece)
+            float had[S::TN][16];
+#pragma unroll
+            for (int y = 0; y < S::TN; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) had[y][v] = out[(size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32];
+#pragma unroll
+            for (int y = 0; y < S::TN; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[x][y][v] += had[y][v];
+        }
 #pragma unroll
         for (int y = 0; y < S::TN; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                float* const o = out + (size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32;
-                *o = add ? *o + acc[x][y][v] : acc[x][y][v];
-            }
+            for (int v = 0; v < 16; ++v) out[(size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32] = acc[x][y][v];
+    }
 }
 
 // The sum of four neighboring cells over the slabs, for SL lanes that share the cells: lane 0 of them has it.
