@@ -141,6 +141,9 @@ namespace {
 constexpr int64_t kMostXentRows = (int64_t)1 << 30;
 constexpr int32_t kMostXentFeatures = 1 << 16, kMostXentClasses = 1 << 22;
 
+// most columns of a checkpoint: offsets within a row are 32 bits
+constexpr int32_t kMostCheckpointCols = 1 << 28;
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int elem_size(int dtype) { return dtype == MIXGCN_BF16 ? 2 : 4; }
@@ -591,6 +594,7 @@ static int check_checkpoint(const char* what, const int8_t* codes, int64_t ld_co
 {
     const std::string who(what);
     if (n_rows < 0 || n_cols <= 0) return fail(MIXGCN_EINVAL, who + ": sizes");
+    if (n_cols > kMostCheckpointCols) return fail(MIXGCN_EUNSUPPORTED, who + ": more than 2^28 columns");
     if (n_rows == 0) return MIXGCN_OK;
     MIXGCN_TRY(check_matrix((who + ": codes").c_str(), codes, ld_codes, n_cols, 1));
     if (!exponents) return fail(MIXGCN_EINVAL, who + ": exponents: null pointer");

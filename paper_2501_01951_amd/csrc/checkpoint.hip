@@ -25,24 +25,48 @@ struct Lane {
     static constexpr int VEC = BF16 ? 8 : 4;      // columns of a lane: 16 bytes of features
     static constexpr int LANES = kGroup / VEC;    // lanes of a group
     static constexpr int ITEMS = kBlock / LANES;  // groups that a block works on at a time
+    static constexpr int ES = BF16 ? 2 : 4;
     using Codes = typename std::conditional<BF16, uint2, uint32_t>::type;
 };
 
-// A block takes rows_per_block rows, and of these a group of columns per `LANES` lanes, four at a time.
+// A block takes rows_per_block rows, and of these a group of columns per `LANES` lanes, four at a time.  Offsets within
+// the rows of a block are 32 bits.
 struct Plan {
     int groups;          // per row
     int rows_per_block;
-    uint32_t magic;      // item / groups = umulhi(item, magic) where a block has several rows
+    uint32_t magic;      // item / groups = umulhi(item, magic) where a block has several rows of several groups
 };
 
-__device__ inline void split_item(const Plan& p, uint32_t item, int* row, int* group)
+__device__ inline void split_item(const Plan& p, uint32_t item, uint32_t* row, uint32_t* group)
 {
-    const uint32_t r = p.groups == 1 ? item : p.rows_per_block > 1 ? __umulhi(item, p.magic) : 0u;
-    *row = (int)r;
-    *group = (int)(item - r * (uint32_t)p.groups);
+    *row = p.groups == 1 ? item : p.rows_per_block > 1 ? __umulhi(item, p.magic) : 0u;
+    *group = item - *row * (uint32_t)p.groups;
 }
 
-// What bounds it: memory, features in and codes out.
+// The largest value of the lanes of a group.
+template <int LANES>
+__device__ inline float group_most(float v)
+{
+    auto other = [](float x, auto ctrl) {
+        const int i = __float_as_int(x);
+        return __int_as_float(__builtin_amdgcn_update_dpp(i, i, decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    v = fmaxf(v, other(v, std::integral_constant<int, 0xB1>{}));   // lane ^ 1
+    v = fmaxf(v, other(v, std::integral_constant<int, 0x4E>{}));   // lane ^ 2
+    if (LANES == 8) v = fmaxf(v, other(v, std::integral_constant<int, 0x141>{}));  // the other four of eight
+    return v;
+}
+
+// The smallest step that holds the largest magnitude of a group.
+__device__ inline int step_for(float top)
+{
+    int s = (int)(__float_as_uint(top) >> 23) - 127 - 6;
+    if (ldexpf(top, -s) >= 127.5f) ++s;
+    return s < -kStepBias ? -kStepBias : s;
+}
+
+// What bounds it: memory, features in and codes out (2^20 x 256 fp32, 1.34 GB: 302 us with a comparison and two selections
+// for every element, PACK_F32 with those only where a wavefront meets something that is not finite).
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void pack_kernel(const void* __restrict__ X, int64_t ldx, int64_t n, int cols,
                                                       int8_t* __restrict__ codes, int64_t ldq,
@@ -53,73 +77,97 @@ __global__ __launch_bounds__(kBlock) void pack_kernel(const void* __restrict__ X
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
     const int rows = n - row0 < p.rows_per_block ? (int)(n - row0) : p.rows_per_block;
     const uint32_t items = (uint32_t)rows * (uint32_t)p.groups;
-    const int sub = threadIdx.x % L::LANES;
+    const uint32_t sub = threadIdx.x % L::LANES;
+    const char* const xb = (const char*)X + row0 * ldx * L::ES;
+    int8_t* const qb = codes + row0 * ldq;
+    uint8_t* const eb = steps + row0 * lde;
+    const uint32_t xp = (uint32_t)ldx * L::ES, qp = (uint32_t)ldq, ep = (uint32_t)lde;
+    const uint32_t padded = (uint32_t)(cols + 15) / 16 * 16;
     for (uint32_t i0 = threadIdx.x / L::LANES; i0 < items; i0 += U * L::ITEMS) {
         uint4 v[U];
-        int row[U], group[U];
+        uint32_t row[U], group[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t i = i0 + u * L::ITEMS;
             split_item(p, i < items ? i : i0, &row[u], &group[u]);
-            const int c = group[u] * kGroup + sub * L::VEC;
+            const uint32_t c = group[u] * kGroup + sub * L::VEC;
             // a lane past the columns reads the row's first ones; its elements are masked below
-            const int cc = c < cols ? c : 0;
-            const char* const x = (const char*)X + ((row0 + row[u]) * ldx + cc) * (BF16 ? 2 : 4);
-            v[u] = *reinterpret_cast<const uint4*>(x);
+            v[u] = *reinterpret_cast<const uint4*>(xb + row[u] * xp + (c < (uint32_t)cols ? c : 0u) * L::ES);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = group[u] * kGroup + sub * L::VEC;
+            const uint32_t c = group[u] * kGroup + sub * L::VEC;
             float f[L::VEC];
             const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
 #pragma unroll
-            for (int e = 0; e < L::VEC; ++e) {
+            for (int e = 0; e < L::VEC; ++e)
                 f[e] = BF16 ? ((e & 1) ? high_half(w[e / 2]) : low_half(w[e / 2])) : __uint_as_float(w[e % 4]);
-                if (c + e >= cols) f[e] = 0.f;
-            }
-            // magnitudes as integers order as the numbers do; those that are not finite do not count
-            uint32_t top = 0;
+            if (c + L::VEC > (uint32_t)cols)
+#pragma unroll
+                for (int e = 0; e < L::VEC; ++e)
+                    if (c + e >= (uint32_t)cols) f[e] = 0.f;
+            float top = 0.f, wild = 0.f;
 #pragma unroll
             for (int e = 0; e < L::VEC; ++e) {
-                const uint32_t m = __float_as_uint(f[e]) & 0x7FFFFFFFu;
-                const uint32_t mm = m < 0x7F800000u ? m : 0u;
-                top = mm > top ? mm : top;
+                top = fmaxf(top, fabsf(f[e]));
+                wild = fmaf(f[e], 0.f, wild);  // NaN after something that is not finite
             }
+            uint32_t bad = 0;
+            if (__builtin_expect(__any(!(wild == 0.f)), 0)) {
+                top = 0.f;
 #pragma unroll
-            for (int o = 1; o < L::LANES; o <<= 1) {
-                const uint32_t t = __shfl_xor(top, o, kWave);
-                top = t > top ? t : top;
+                for (int e = 0; e < L::VEC; ++e) {
+                    if (fabsf(f[e]) <= 3.402823466e38f) {
+                        top = fmaxf(top, fabsf(f[e]));
+                    } else {
+                        bad |= 1u << e;
+                        f[e] = 0.f;
+                    }
+                }
             }
-            int s = (int)(top >> 23) - 127 - 6;
-            if (ldexpf(__uint_as_float(top), -s) >= 127.5f) ++s;
-            if (s < -kStepBias) s = -kStepBias;
+            const int s = step_for(group_most<L::LANES>(top));
             uint32_t out[L::VEC / 4];
 #pragma unroll
             for (int q = 0; q < L::VEC / 4; ++q) {
-                out[q] = 0;
+                uint32_t code[4];
+                // the sum is rounded to a whole number, to even in a tie, and has it in its low bits
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const float x = f[4 * q + b];
-                    const bool finite = (__float_as_uint(x) & 0x7FFFFFFFu) < 0x7F800000u;
-                    const int code = finite ? (int)rintf(ldexpf(x, -s)) : -128;
-                    out[q] |= ((uint32_t)code & 255u) << (8 * b);
-                }
+                for (int b = 0; b < 4; ++b) code[b] = __float_as_uint(ldexpf(f[4 * q + b], -s) + 12582912.f);
+                out[q] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(code[3], code[2], 0x0c0c0400u),
+                                               __builtin_amdgcn_perm(code[1], code[0], 0x0c0c0400u), 0x05040100u);
+                if (__builtin_expect(bad != 0, 0))
+                    for (int b = 0; b < 4; ++b)
+                        if (bad >> (4 * q + b) & 1u) out[q] = (out[q] & ~(255u << (8 * b))) | 128u << (8 * b);
             }
             if (i0 + u * L::ITEMS >= items) continue;
-            const int64_t r = row0 + row[u];
             // the row's padding up to whole 16 bytes becomes zero
-            if (c < (cols + 15) / 16 * 16) {
+            if (c < padded) {
                 typename L::Codes o;
                 __builtin_memcpy(&o, out, sizeof(o));
-                *reinterpret_cast<typename L::Codes*>(codes + r * ldq + c) = o;
+                *reinterpret_cast<typename L::Codes*>(qb + (row[u] * qp + c)) = o;
             }
-            if (sub == 0) steps[r * lde + group[u]] = (uint8_t)(s + kStepBias);
+            if (sub == 0) eb[row[u] * ep + group[u]] = (uint8_t)(s + kStepBias);
         }
     }
 }
 
 // What a code stands for.
 __device__ inline float value_of(int code, float step) { return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step; }
+// whether one of four codes is -128
+__device__ inline bool has_bad(uint32_t w)
+{
+    const uint32_t t = w ^ 0x80808080u;
+    return ((t - 0x01010101u) & ~t & 0x80808080u) != 0;
+}
+// What four codes stand for.
+__device__ inline void values_of(uint32_t w, float step, float* f)
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) f[b] = (float)(int8_t)(w >> (8 * b)) * step;
+    if (__builtin_expect(has_bad(w), 0))
+#pragma unroll
+        for (int b = 0; b < 4; ++b) f[b] = value_of((int8_t)(w >> (8 * b)), step);
+}
 
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void unpack_kernel(const int8_t* __restrict__ codes, int64_t ldq,
@@ -131,49 +179,54 @@ __global__ __launch_bounds__(kBlock) void unpack_kernel(const int8_t* __restrict
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
     const int rows = n - row0 < p.rows_per_block ? (int)(n - row0) : p.rows_per_block;
     const uint32_t items = (uint32_t)rows * (uint32_t)p.groups;
-    const int sub = threadIdx.x % L::LANES;
+    const uint32_t sub = threadIdx.x % L::LANES;
+    char* const xb = (char*)X + row0 * ldx * L::ES;
+    const int8_t* const qb = codes + row0 * ldq;
+    const uint8_t* const eb = steps + row0 * lde;
+    const uint32_t xp = (uint32_t)ldx * L::ES, qp = (uint32_t)ldq, ep = (uint32_t)lde;
     for (uint32_t i0 = threadIdx.x / L::LANES; i0 < items; i0 += U * L::ITEMS) {
         typename L::Codes v[U];
-        uint32_t e[U];
-        int row[U], group[U];
+        uint32_t e[U], row[U], group[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t i = i0 + u * L::ITEMS;
             split_item(p, i < items ? i : i0, &row[u], &group[u]);
-            const int c = group[u] * kGroup + sub * L::VEC;
-            const int cc = c < cols ? c : 0;
-            v[u] = *reinterpret_cast<const typename L::Codes*>(codes + (row0 + row[u]) * ldq + cc);
-            e[u] = steps[(row0 + row[u]) * lde + group[u]];
+            const uint32_t c = group[u] * kGroup + sub * L::VEC;
+            v[u] = *reinterpret_cast<const typename L::Codes*>(qb + (row[u] * qp + (c < (uint32_t)cols ? c : 0u)));
+            e[u] = eb[row[u] * ep + group[u]];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = group[u] * kGroup + sub * L::VEC;
-            if (i0 + u * L::ITEMS >= items || c >= cols) continue;
+            const uint32_t c = group[u] * kGroup + sub * L::VEC;
+            if (i0 + u * L::ITEMS >= items || c >= (uint32_t)cols) continue;
             const float step = step_of(e[u]);
             uint32_t w[L::VEC / 4];
             __builtin_memcpy(w, &v[u], sizeof(w));
             float f[L::VEC];
 #pragma unroll
-            for (int b = 0; b < L::VEC; ++b) f[b] = value_of((int8_t)(w[b / 4] >> (8 * (b % 4))), step);
+            for (int q = 0; q < L::VEC / 4; ++q) values_of(w[q], step, f + 4 * q);
             uint32_t o[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 o[q] = BF16 ? (__float_as_uint(f[(2 * q) % L::VEC]) >> 16) | (__float_as_uint(f[(2 * q + 1) % L::VEC]) & 0xFFFF0000u)
                             : __float_as_uint(f[q]);
-            char* const x = (char*)X + ((row0 + row[u]) * ldx + c) * (BF16 ? 2 : 4);
-            if (c + L::VEC <= cols) {
+            char* const x = xb + (row[u] * xp + c * L::ES);
+            if (c + L::VEC <= (uint32_t)cols) {
                 *reinterpret_cast<uint4*>(x) = make_uint4(o[0], o[1], o[2], o[3]);
             } else {
-                for (int b = 0; c + b < cols; ++b) {
-                    if (BF16) ((uint16_t*)x)[b] = (uint16_t)(__float_as_uint(f[b]) >> 16);
-                    else ((float*)x)[b] = f[b];
-                }
+#pragma unroll
+                for (int b = 0; b < L::VEC; ++b)
+                    if (c + b < (uint32_t)cols) {
+                        if (BF16) ((uint16_t*)x)[b] = (uint16_t)(__float_as_uint(f[b]) >> 16);
+                        else ((float*)x)[b] = f[b];
+                    }
             }
         }
     }
 }
 
-Plan plan_rows(int64_t n, int cols, int items)
+// row_bytes: the largest pitch of the row-wise arrays
+Plan plan_rows(int64_t n, int cols, int items, int64_t row_bytes)
 {
     Plan p;
     p.groups = (int)ceil_div(cols, kGroup);
@@ -183,28 +236,53 @@ Plan plan_rows(int64_t n, int cols, int items)
     const int64_t least = ceil_div(items, p.groups), most = 32 * items / p.groups;
     if (rows > most) rows = most;
     if (rows < least) rows = least;
+    if (rows > (((int64_t)1 << 31) - 1) / row_bytes) rows = (((int64_t)1 << 31) - 1) / row_bytes;
+    if (rows < 1) rows = 1;
     p.rows_per_block = (int)rows;
     p.magic = p.groups > 1 ? (uint32_t)(((1ull << 32) + p.groups - 1) / p.groups) : 0u;
     return p;
 }
 
+int64_t longest_row(int64_t ldx, int es, int64_t ldq, int64_t lde)
+{
+    int64_t b = ldx * es;
+    if (ldq > b) b = ldq;
+    return lde > b ? lde : b;
+}
+
 // ---- weight gradient ----------------------------------------------------------------------------
 // P[slab][KD x MD] = Z8[rows of slab][KD]^T * (G (.) M)[rows][MD].  Z8 is one bf16 term; bf16 gradients are too, and
 // fp32 ones the exact sum of three, taken times 2^16 so that the terms of every float are bf16 numbers.
+//
+// A workgroup has 128 x 64 TN cells on 2 x 2 wavefronts and walks its rows 32 at a time.  Global loads run two steps ahead in two
+// register sets, LDS is double buffered, one barrier per step: decoding and splitting the next step and the products of
+// this one do not wait for each other.  The tiles lie in LDS as in memory, row by row, and the LDS read transposes; of
+// a row of 128 (64) columns the 64-byte block q is at q ^ (row % 4) (row / 2 % 2), so that the four rows that are read
+// together come from all banks.
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
-constexpr int BKS = 16;         // rows per step, the reduction depth of an MFMA
-constexpr int LDW = 128 + 32;   // halfwords per staged row
-constexpr int kTile = BKS * LDW;
+constexpr int BKS = 32;  // rows per step
 
-// Lane i of 16 receives element i % 4 of the 8 bytes that lanes i / 4, + 4, + 8 and + 12 address: with lane s of the
-// group at row s / 4, features 4 (s % 4) .. + 3, every lane has its own feature at four consecutive rows.
-__device__ inline bf16x8 read_transposed(const uint16_t* p)
+// halfwords of (row, column) of a tile of WIDTH columns
+template <int WIDTH>
+__device__ inline int place(int row, int col)
 {
+    const int block = col / 32 ^ (WIDTH == 128 ? row & 3 : row >> 1 & 1);
+    return row * WIDTH + block * 32 + col % 32;
+}
+
+// Operand of the 32 columns from col0 on and 16 rows from row0 on.  Lane i of 16 receives element i % 4 of the 8 bytes that
+// lanes i / 4, + 4, + 8 and + 12 address: with lane s of the group at row s / 4, columns 4 (s % 4) .. + 3, every lane has
+// its own column at four consecutive rows.
+template <int WIDTH>
+__device__ inline bf16x8 read_transposed(const uint16_t* tile, int col0, int row0, int lane)
+{
+    const int grp = lane >> 4, gs = lane & 15;
+    const uint16_t* const p = tile + place<WIDTH>(row0 + 8 * (grp >> 1) + (gs >> 2), col0 + 16 * (grp & 1) + 4 * (gs & 3));
     const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)p);
-    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * LDW));
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * WIDTH));
     const shortx8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     bf16x8 o;
     __builtin_memcpy(&o, &v, 16);
@@ -214,125 +292,157 @@ __device__ inline bf16x8 read_transposed(const uint16_t* p)
 // four codes as two words of bf16
 __device__ inline uint2 decode4(uint32_t w, float step)
 {
-    uint32_t f[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) f[b] = __float_as_uint(value_of((int8_t)(w >> (8 * b)), step));
-    return make_uint2((f[0] >> 16) | (f[1] & 0xFFFF0000u), (f[2] >> 16) | (f[3] & 0xFFFF0000u));
+    float f[4];
+    values_of(w, step, f);
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u));
 }
 
-template <bool BF16, bool MASK>
+template <bool BF16, bool MASK, int TN>
 __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     const int8_t* __restrict__ codes, int64_t ldq, const uint8_t* __restrict__ steps, int64_t lde,
     const void* __restrict__ G, int64_t ldg, const uint32_t* __restrict__ mask, int64_t ldm, float* __restrict__ P,
     int KD, int MD, int64_t rows_per_slab, int64_t n_rows, int n_i_tiles, int n_j_tiles)
 {
-    constexpr int PLANES = BF16 ? 1 : 3;
-    constexpr int ES = BF16 ? 2 : 4;
-    __shared__ __attribute__((aligned(16))) uint16_t As[2][kTile];
-    __shared__ __attribute__((aligned(16))) uint16_t Bs[2][PLANES * kTile];
+    constexpr int PLANES = BF16 ? 1 : 3, ES = BF16 ? 2 : 4;
+    constexpr int WB = 64 * TN;            // columns of G in a tile
+    constexpr int PER_ROW = WB / 8;        // threads to a row of G
+    constexpr int PB = BKS * PER_ROW / kBlock;  // rows of G per thread and step
+    constexpr int APLANE = BKS * 128, BPLANE = BKS * WB;
+    __shared__ __attribute__((aligned(16))) uint16_t As[2][APLANE];
+    __shared__ __attribute__((aligned(16))) uint16_t Bs[2][PLANES * BPLANE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / 2, wn = wave % 2;
     const int tiles = n_i_tiles * n_j_tiles;
     const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int64_t slab = lid / (unsigned)tiles;
-    const int t = (int)(lid % (unsigned)tiles);
-    const int i0 = (t / n_j_tiles) * 128, j0 = (t % n_j_tiles) * 128;
+    const int slab = __builtin_amdgcn_readfirstlane((int)(lid / (unsigned)tiles));
+    const int t = __builtin_amdgcn_readfirstlane((int)(lid % (unsigned)tiles));
+    const int i0 = (t / n_j_tiles) * 128, j0 = (t % n_j_tiles) * WB;
     const int64_t r_begin = slab * rows_per_slab;
     const int64_t r_end = r_begin + rows_per_slab < n_rows ? r_begin + rows_per_slab : n_rows;
-    const int nk = r_end > r_begin ? (int)((r_end - r_begin + BKS - 1) / BKS) : 0;
+    const int n_here = (int)(r_end - r_begin), nk = (n_here + BKS - 1) / BKS;
 
-    floatx16 acc[2][2];
+    floatx16 acc[2][TN];
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < TN; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
 
-    // staging: a thread takes eight columns of a row, of Z8 and of G.  Columns past the matrices reach only cells that
-    // are not stored: any column of the row will do.
-    const int row = tid >> 4, col = 8 * (tid & 15);
-    const int acol = i0 + col < KD ? i0 + col : i0, bcol = j0 + col < MD ? j0 + col : j0;
-    // the last eight codes of a row may lie half past its pitch only where the pitch is not whole: it is
-    const int8_t* const a0 = codes + acol;
-    const uint8_t* const e0 = steps + acol / kGroup;
-    const char* const b0 = (const char*)G + (int64_t)bcol * ES;
-    const uint32_t* const m0 = MASK ? mask + bcol / 32 : nullptr;
+    // staging: a thread takes 16 codes of a row and eight columns of PB rows of G.  Columns past the matrices reach
+    // only cells that are not stored: any column of the row will do.
+    const int arow = tid >> 3, acol = 16 * (tid & 7);
+    const int brow = tid / PER_ROW, bcol = 8 * (tid % PER_ROW);
+    const int ka = i0 + acol < KD ? i0 + acol : i0, mb = j0 + bcol < MD ? j0 + bcol : j0;
+    const int8_t* const a0 = codes + r_begin * ldq + ka;
+    const uint8_t* const e0 = steps + r_begin * lde + ka / kGroup;
+    const char* const b0 = (const char*)G + (r_begin * ldg + mb) * ES;
+    const uint32_t* const m0 = MASK ? mask + r_begin * ldm + mb / 32 : nullptr;
+    const bool wide = BF16 || mb + 4 < ldg;  // the second four columns exist where the pitch has them
     struct Regs {
-        uint2 a;
-        uint4 b[BF16 ? 1 : 2];
-        uint32_t e, m;
-    } g;
-    auto load = [&](int step) {
-        const int64_t r = r_begin + (int64_t)step * BKS + row;
-        const bool in = r < r_end;
-        const int64_t rr = in ? r : r_begin;
-        g.a = *reinterpret_cast<const uint2*>(a0 + rr * ldq);
-        g.e = e0[rr * lde];
-        const uint4* const b = reinterpret_cast<const uint4*>(b0 + rr * ldg * ES);
-        g.b[0] = b[0];
-        // (fp32: the second four columns exist where the pitch has them)
-        if (!BF16) g.b[BF16 ? 0 : 1] = bcol + 4 < ldg ? b[1] : b[0];
-        g.m = MASK ? m0[rr * ldm] : 0xFFFFFFFFu;
-        if (MASK) g.m >>= bcol % 32;
-        if (!in) {
-            g.a = make_uint2(0u, 0u);
-            g.m = 0u;
+        uint4 a, b[PB][BF16 ? 1 : 2];
+        uint32_t e, m[MASK ? PB : 1];
+    };
+    // every load of every step is issued; rows past the slab's end are its last one, and zeroed on their way to LDS
+    auto load = [&](Regs& g, int step) {
+        const int ra = step * BKS + arow < n_here ? step * BKS + arow : n_here - 1;
+        g.a = *reinterpret_cast<const uint4*>(a0 + ra * ldq);
+        g.e = e0[ra * lde];
+#pragma unroll
+        for (int p = 0; p < PB; ++p) {
+            const int rb = step * BKS + brow + p * (BKS / PB) < n_here ? step * BKS + brow + p * (BKS / PB) : n_here - 1;
+            const char* const b = b0 + rb * ldg * ES;
+            g.b[p][0] = *reinterpret_cast<const uint4*>(b);
+            if (!BF16) g.b[p][BF16 ? 0 : 1] = *reinterpret_cast<const uint4*>(b + (wide ? 16 : 0));
+            if (MASK) g.m[MASK ? p : 0] = m0[rb * ldm];
         }
     };
-    auto store = [&](uint16_t* as, uint16_t* bs) {
-        const float step = step_of(g.e);
-        const uint2 lo = decode4(g.a.x, step), hi = decode4(g.a.y, step);
-        lds_store16(as + row * LDW + col, make_uint4(lo.x, lo.y, hi.x, hi.y));
-        uint16_t* const q = bs + row * LDW + col;
-        if (BF16) {
-            uint32_t w[4] = {g.b[0].x, g.b[0].y, g.b[0].z, g.b[0].w};
+    auto store = [&](const Regs& g, int step, uint16_t* as, uint16_t* bs) {
+        const bool whole = (step + 1) * BKS <= n_here;
+        uint4 a = g.a;
+        if (!whole && step * BKS + arow >= n_here) a = make_uint4(0u, 0u, 0u, 0u);
+        const float unit = step_of(g.e);
+        const uint2 d0 = decode4(a.x, unit), d1 = decode4(a.y, unit), d2 = decode4(a.z, unit), d3 = decode4(a.w, unit);
+        uint16_t* const q = as + place<128>(arow, acol);
+        lds_store16(q, make_uint4(d0.x, d0.y, d1.x, d1.y));
+        lds_store16(q + 8, make_uint4(d2.x, d2.y, d3.x, d3.y));
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] &= ((g.m >> (2 * i)) & 1u ? 0xFFFFu : 0u) | ((g.m >> (2 * i)) & 2u ? 0xFFFF0000u : 0u);
-            lds_store16(q, make_uint4(w[0], w[1], w[2], w[3]));
-        } else {
+        for (int p = 0; p < PB; ++p) {
+            const int r = brow + p * (BKS / PB);
+            uint32_t m = MASK ? g.m[MASK ? p : 0] >> (mb % 32) : 0xFFu;
+            if (!whole && step * BKS + r >= n_here) m = 0u;
+            uint16_t* const o = bs + place<WB>(r, bcol);
+            if (BF16) {
+                const uint4 v = g.b[p][0];
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                if (MASK || !whole)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 u = g.b[BF16 ? 0 : h];
-                const uint32_t m = g.m >> (4 * h);
-                float4 x;
-                x.x = m & 1u ? __uint_as_float(u.x) : 0.f;
-                x.y = m & 2u ? __uint_as_float(u.y) : 0.f;
-                x.z = m & 4u ? __uint_as_float(u.z) : 0.f;
-                x.w = m & 8u ? __uint_as_float(u.w) : 0.f;
-                split_store<false>(x, x, kTermScale, q + 4 * h, q + kTile + 4 * h, q + 2 * kTile + 4 * h);
+                    for (int i = 0; i < 4; ++i)
+                        w[i] &= ((uint32_t)((int32_t)(m << (31 - 2 * i)) >> 31) & 0xFFFFu) |
+                                ((uint32_t)((int32_t)(m << (30 - 2 * i)) >> 31) & 0xFFFF0000u);
+                lds_store16(o, make_uint4(w[0], w[1], w[2], w[3]));
+            } else {
+                const uint4 v0 = g.b[p][0], v1 = g.b[p][BF16 ? 0 : 1];
+                uint32_t w[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+                if (MASK || !whole)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] &= (uint32_t)((int32_t)(m << (31 - i)) >> 31);
+                uint32_t term[3][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = __uint_as_float(w[2 * i]) * kTermScale, y = __uint_as_float(w[2 * i + 1]) * kTermScale;
+#pragma unroll
+                    for (int s = 0; s < 3; ++s) {
+                        term[s][i] = pack_bf16(x, y);
+                        x -= low_half(term[s][i]);
+                        y -= high_half(term[s][i]);
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 3; ++s)
+                    lds_store16(o + (BF16 ? 0 : s) * BPLANE, make_uint4(term[s][0], term[s][1], term[s][2], term[s][3]));
             }
         }
     };
-    const int grp = lane >> 4, gs = lane & 15;
-    const int rpos = (8 * (grp >> 1) + (gs >> 2)) * LDW + 16 * (grp & 1) + 4 * (gs & 3);
     auto mma = [&](const uint16_t* as, const uint16_t* bs) {
-        bf16x8 a[2], b[2][PLANES];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            a[x] = read_transposed(as + rpos + (wm * 2 + x) * 32);
+        for (int kc = 0; kc < BKS; kc += 16) {
+            bf16x8 a[2], b[TN][PLANES];
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) b[x][p] = read_transposed(bs + p * kTile + rpos + (wn * 2 + x) * 32);
+            for (int x = 0; x < 2; ++x) a[x] = read_transposed<128>(as, (wm * 2 + x) * 32, kc, lane);
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) b[y][p] = read_transposed<WB>(bs + p * BPLANE, (wn * TN + y) * 32, kc, lane);
+            // the smaller products first
+#pragma unroll
+            for (int p = PLANES - 1; p >= 0; --p)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < TN; ++y)
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[y][p], acc[x][y], 0, 0, 0);
         }
-#pragma unroll
-        for (int p = PLANES - 1; p >= 0; --p)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[y][p], acc[x][y], 0, 0, 0);
     };
     if (nk > 0) {
-        load(0);
-        store(As[0], Bs[0]);
+        Regs g0, g1;
+        load(g0, 0);
+        load(g1, 1);
+        store(g0, 0, As[0], Bs[0]);
+        load(g0, 2);
         __syncthreads();
-        for (int i = 0; i < nk; ++i) {
-            if (i + 1 < nk) load(i + 1);
-            mma(As[i & 1], Bs[i & 1]);
-            if (i + 1 < nk) store(As[(i + 1) & 1], Bs[(i + 1) & 1]);
+        for (int i = 0; i + 1 < nk; i += 2) {
+            store(g1, i + 1, As[1], Bs[1]);
+            load(g1, i + 3);
+            mma(As[0], Bs[0]);
+            __syncthreads();
+            store(g0, i + 2, As[0], Bs[0]);
+            load(g0, i + 4);
+            mma(As[1], Bs[1]);
             __syncthreads();
         }
+        if (nk & 1) mma(As[0], Bs[0]);
     }
 
     // D layout: lane l, register v -> row 8 (v / 4) + 4 (l / 32) + v % 4, col l % 32
@@ -342,8 +452,8 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int j = j0 + (wn * 2 + y) * 32 + li;
+        for (int y = 0; y < TN; ++y) {
+            const int j = j0 + (wn * TN + y) * 32 + li;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int i = i0 + (wm * 2 + x) * 32 + 8 * (v / 4) + 4 * lk + (v % 4);
@@ -366,13 +476,14 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
 
 struct Slabs {
     int64_t n, rows;
-    int nit, njt;
+    int nit, njt, width;
 };
 Slabs plan_slabs(int64_t n, int32_t k, int32_t m)
 {
     Slabs s;
     s.nit = (int)ceil_div(k, 128);
-    s.njt = (int)ceil_div(m, 128);
+    s.width = m > 64 ? 128 : 64;
+    s.njt = (int)ceil_div(m, s.width);
     s.n = wgrad_slabs(n, (int64_t)s.nit * s.njt, 1024);
     s.rows = ceil_div(ceil_div(n, s.n), BKS) * BKS;
     if (s.rows < BKS) s.rows = BKS;
@@ -387,7 +498,7 @@ int launch_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n, int
 {
     if (n == 0) return MIXGCN_OK;
     const bool bf16 = dtype == MIXGCN_BF16;
-    const Plan p = plan_rows(n, cols, bf16 ? Lane<true>::ITEMS : Lane<false>::ITEMS);
+    const Plan p = plan_rows(n, cols, bf16 ? Lane<true>::ITEMS : Lane<false>::ITEMS, longest_row(ldx, bf16 ? 2 : 4, ldq, lde));
     const int64_t grid = ceil_div(n, p.rows_per_block);
     if (grid > 0x7FFFFFFF) return fail(MIXGCN_EINVAL, "checkpoint_pack: too many rows");
     if (bf16)
@@ -405,7 +516,7 @@ int launch_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ldq, const 
 {
     if (n == 0) return MIXGCN_OK;
     const bool bf16 = dtype == MIXGCN_BF16;
-    const Plan p = plan_rows(n, cols, bf16 ? Lane<true>::ITEMS : Lane<false>::ITEMS);
+    const Plan p = plan_rows(n, cols, bf16 ? Lane<true>::ITEMS : Lane<false>::ITEMS, longest_row(ldx, bf16 ? 2 : 4, ldq, lde));
     const int64_t grid = ceil_div(n, p.rows_per_block);
     if (grid > 0x7FFFFFFF) return fail(MIXGCN_EINVAL, "checkpoint_unpack: too many rows");
     if (bf16)
@@ -429,10 +540,16 @@ int launch_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ldq, const u
 {
     const Slabs p = plan_slabs(n, k, m);
     const int64_t grid = p.n * p.nit * p.njt;
-    if (grid > 0x7FFFFFFF) return fail(MIXGCN_EINVAL, "checkpoint_wgrad: too many tiles");
-#define MIXGCN_WGRAD8(BF16, MASK)                                                                                    \
-    hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, ldq,  \
-                       steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt)
+    if (grid > 0x7FFFFFFF || p.rows > (1 << 30)) return fail(MIXGCN_EUNSUPPORTED, "checkpoint_wgrad: too many tiles or rows");
+#define MIXGCN_WGRAD8(BF16, MASK)                                                                                         \
+    do {                                                                                                                  \
+        if (p.width == 128)                                                                                               \
+            hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK, 2>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, \
+                               ldq, steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt);                     \
+        else                                                                                                              \
+            hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK, 1>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, \
+                               ldq, steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt);                     \
+    } while (0)
     if (dtype == MIXGCN_BF16) {
         if (mask) MIXGCN_WGRAD8(true, true);
         else MIXGCN_WGRAD8(true, false);
