@@ -451,6 +451,7 @@ int mixgcn_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ld_codes, c
  * fp32, beta 0 or 1.  The values of Z and bf16 gradients enter the bf16 matrix cores as they are, fp32 gradients
  * as the exact sum of three bf16 terms; sums are fp32, and those of the row slabs are joined in 64 bits in a fixed
  * order.  Infinities and NaN give what fp32 arithmetic gives.  What a masked element of G holds does not matter.
+ * Pitches are below 2^26 bytes.
  *   workspace : device memory of mixgcn_checkpoint_wgrad_workspace(n_rows, k, m) bytes (-1 for bad sizes), 16-byte
  *   aligned, which the call uses until its work on the stream is done.  The call allocates nothing and does not
  *   synchronise.

@@ -153,20 +153,21 @@ __global__ __launch_bounds__(kBlock) void pack_kernel(const void* __restrict__ X
 
 // What a code stands for.
 __device__ inline float value_of(int code, float step) { return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step; }
-// whether one of four codes is -128
-__device__ inline bool has_bad(uint32_t w)
+// What the codes of N words stand for.  (-128 is the least code, so that the least of them tells whether it is there.)
+template <int N>
+__device__ inline void values_of(const uint32_t (&w)[N], float step, float (&f)[4 * N])
 {
-    const uint32_t t = w ^ 0x80808080u;
-    return ((t - 0x01010101u) & ~t & 0x80808080u) != 0;
-}
-// What four codes stand for.
-__device__ inline void values_of(uint32_t w, float step, float* f)
-{
+    float least = 0.f;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) f[b] = (float)(int8_t)(w >> (8 * b)) * step;
-    if (__builtin_expect(has_bad(w), 0))
+    for (int b = 0; b < 4 * N; ++b) {
+        f[b] = (float)(int8_t)(w[b / 4] >> (8 * (b % 4)));
+        least = fminf(least, f[b]);
+    }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) f[b] = value_of((int8_t)(w >> (8 * b)), step);
+    for (int b = 0; b < 4 * N; ++b) f[b] *= step;
+    if (__builtin_expect(least == -128.f, 0))
+#pragma unroll
+        for (int b = 0; b < 4 * N; ++b) f[b] = value_of((int8_t)(w[b / 4] >> (8 * (b % 4))), step);
 }
 
 template <bool BF16>
@@ -203,8 +204,7 @@ __global__ __launch_bounds__(kBlock) void unpack_kernel(const int8_t* __restrict
             uint32_t w[L::VEC / 4];
             __builtin_memcpy(w, &v[u], sizeof(w));
             float f[L::VEC];
-#pragma unroll
-            for (int q = 0; q < L::VEC / 4; ++q) values_of(w[q], step, f + 4 * q);
+            values_of(w, step, f);
             uint32_t o[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -214,12 +214,19 @@ __global__ __launch_bounds__(kBlock) void unpack_kernel(const int8_t* __restrict
             if (c + L::VEC <= (uint32_t)cols) {
                 *reinterpret_cast<uint4*>(x) = make_uint4(o[0], o[1], o[2], o[3]);
             } else {
-#pragma unroll
-                for (int b = 0; b < L::VEC; ++b)
-                    if (c + b < (uint32_t)cols) {
-                        if (BF16) ((uint16_t*)x)[b] = (uint16_t)(__float_as_uint(f[b]) >> 16);
-                        else ((float*)x)[b] = f[b];
+                // the last columns, 8, 4 and 2 bytes at a time (one by one they took a third of the time of 100 columns)
+                const uint32_t left = (uint32_t)cols - c;
+                if (BF16) {
+                    if (left & 4u) *reinterpret_cast<uint2*>(x) = make_uint2(o[0], o[1]);
+                    if (left & 2u) *reinterpret_cast<uint32_t*>(x + (left & 4u) * 2) = left & 4u ? o[2] : o[0];
+                    if (left & 1u) {
+                        const uint32_t at = left / 2;
+                        *reinterpret_cast<uint16_t*>(x + 4 * at) = (uint16_t)(at == 0 ? o[0] : at == 1 ? o[1] : at == 2 ? o[2] : o[3]);
                     }
+                } else {
+                    if (left & 2u) *reinterpret_cast<uint2*>(x) = make_uint2(o[0], o[1]);
+                    if (left & 1u) *reinterpret_cast<uint32_t*>(x + (left & 2u) * 4) = left & 2u ? o[2] : o[0];
+                }
             }
         }
     }
@@ -254,10 +261,10 @@ int64_t longest_row(int64_t ldx, int es, int64_t ldq, int64_t lde)
 // P[slab][KD x MD] = Z8[rows of slab][KD]^T * (G (.) M)[rows][MD].  Z8 is one bf16 term; bf16 gradients are too, and
 // fp32 ones the exact sum of three, taken times 2^16 so that the terms of every float are bf16 numbers.
 //
-// A workgroup has 128 x 64 TN cells on 2 x 2 wavefronts and walks its rows 32 at a time.  Global loads run two steps ahead in two
+// A workgroup has 64 TM x 64 TN cells on 2 x 2 wavefronts and walks its rows 32 at a time.  Global loads run two steps ahead in two
 // register sets, LDS is double buffered, one barrier per step: decoding and splitting the next step and the products of
 // this one do not wait for each other.  The tiles lie in LDS as in memory, row by row, and the LDS read transposes; of
-// a row of 128 (64) columns the 64-byte block q is at q ^ (row % 4) (row / 2 % 2), so that the four rows that are read
+// a row of 128 or 256 (64) columns the 64-byte block q is at q ^ (row % 4) (row / 2 % 2), so that the four rows that are read
 // together come from all banks.
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
@@ -269,7 +276,7 @@ constexpr int BKS = 32;  // rows per step
 template <int WIDTH>
 __device__ inline int place(int row, int col)
 {
-    const int block = col / 32 ^ (WIDTH == 128 ? row & 3 : row >> 1 & 1);
+    const int block = col / 32 ^ (WIDTH == 64 ? row >> 1 & 1 : row & 3);
     return row * WIDTH + block * 32 + col % 32;
 }
 
@@ -289,26 +296,28 @@ __device__ inline bf16x8 read_transposed(const uint16_t* tile, int col0, int row
     return o;
 }
 
-// four codes as two words of bf16
-__device__ inline uint2 decode4(uint32_t w, float step)
+__device__ inline uint4 load16(__amdgpu_buffer_rsrc_t rows, uint32_t offset)
 {
-    float f[4];
-    values_of(w, step, f);
-    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
-                      __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u));
+    const uintx4 v = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)offset, 0, 0);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ inline __amdgpu_buffer_rsrc_t rows_at(const char* first, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, bytes, 0x00020000);
 }
 
-template <bool BF16, bool MASK, int TN>
+template <bool BF16, bool MASK, int TM, int TN>
 __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     const int8_t* __restrict__ codes, int64_t ldq, const uint8_t* __restrict__ steps, int64_t lde,
     const void* __restrict__ G, int64_t ldg, const uint32_t* __restrict__ mask, int64_t ldm, float* __restrict__ P,
     int KD, int MD, int64_t rows_per_slab, int64_t n_rows, int n_i_tiles, int n_j_tiles)
 {
     constexpr int PLANES = BF16 ? 1 : 3, ES = BF16 ? 2 : 4;
-    constexpr int WB = 64 * TN;            // columns of G in a tile
+    constexpr int WA = 64 * TM, WB = 64 * TN;  // columns of Z8 and of G in a tile
+    constexpr int PA = BKS * (WA / 16) / kBlock, PER_ROW_A = WA / 16;  // rows of Z8 per thread and step, threads to a row
     constexpr int PER_ROW = WB / 8;        // threads to a row of G
     constexpr int PB = BKS * PER_ROW / kBlock;  // rows of G per thread and step
-    constexpr int APLANE = BKS * 128, BPLANE = BKS * WB;
+    constexpr int APLANE = BKS * WA, BPLANE = BKS * WB;
     __shared__ __attribute__((aligned(16))) uint16_t As[2][APLANE];
     __shared__ __attribute__((aligned(16))) uint16_t Bs[2][PLANES * BPLANE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -317,66 +326,99 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
     const int slab = __builtin_amdgcn_readfirstlane((int)(lid / (unsigned)tiles));
     const int t = __builtin_amdgcn_readfirstlane((int)(lid % (unsigned)tiles));
-    const int i0 = (t / n_j_tiles) * 128, j0 = (t % n_j_tiles) * WB;
+    const int i0 = (t / n_j_tiles) * WA, j0 = (t % n_j_tiles) * WB;
     const int64_t r_begin = slab * rows_per_slab;
     const int64_t r_end = r_begin + rows_per_slab < n_rows ? r_begin + rows_per_slab : n_rows;
     const int n_here = (int)(r_end - r_begin), nk = (n_here + BKS - 1) / BKS;
 
-    floatx16 acc[2][TN];
+    floatx16 acc[TM][TN];
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < TM; ++a)
 #pragma unroll
         for (int b = 0; b < TN; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
 
-    // staging: a thread takes 16 codes of a row and eight columns of PB rows of G.  Columns past the matrices reach
+    // staging: a thread takes 16 codes of PA rows and eight columns of PB rows of G.  Columns past the matrices reach
     // only cells that are not stored: any column of the row will do.
-    const int arow = tid >> 3, acol = 16 * (tid & 7);
+    const int arow = tid / PER_ROW_A, acol = 16 * (tid % PER_ROW_A);
     const int brow = tid / PER_ROW, bcol = 8 * (tid % PER_ROW);
     const int ka = i0 + acol < KD ? i0 + acol : i0, mb = j0 + bcol < MD ? j0 + bcol : j0;
-    const int8_t* const a0 = codes + r_begin * ldq + ka;
-    const uint8_t* const e0 = steps + r_begin * lde + ka / kGroup;
-    const char* const b0 = (const char*)G + (r_begin * ldg + mb) * ES;
-    const uint32_t* const m0 = MASK ? mask + r_begin * ldm + mb / 32 : nullptr;
-    const bool wide = BF16 || mb + 4 < ldg;  // the second four columns exist where the pitch has them
+    const int pq = (int)ldq, pe = (int)lde, pg = (int)(ldg * ES), pm = (int)(ldm * 4);  // pitches in bytes
+    uint32_t aoff[PA], eoff[PA], boff[PB], moff[PB];
+#pragma unroll
+    for (int p = 0; p < PA; ++p) {
+        aoff[p] = (uint32_t)(arow + p * (BKS / PA)) * (uint32_t)pq + (uint32_t)ka;
+        eoff[p] = (uint32_t)(arow + p * (BKS / PA)) * (uint32_t)pe + (uint32_t)(ka / kGroup);
+    }
+#pragma unroll
+    for (int p = 0; p < PB; ++p) {
+        boff[p] = (uint32_t)(brow + p * (BKS / PB)) * (uint32_t)pg + (uint32_t)(mb * ES);
+        moff[p] = (uint32_t)(brow + p * (BKS / PB)) * (uint32_t)pm + (uint32_t)(mb / 32 * 4);
+    }
+    const uint32_t second = !BF16 && mb + 4 < ldg ? 16u : 0u;  // the second four columns exist where the pitch has them
     struct Regs {
-        uint4 a, b[PB][BF16 ? 1 : 2];
-        uint32_t e, m[MASK ? PB : 1];
+        uint4 a[PA], b[PB][BF16 ? 1 : 2];
+        uint32_t e[PA], m[MASK ? PB : 1];
     };
-    // every load of every step is issued; rows past the slab's end are its last one, and zeroed on their way to LDS
-    auto load = [&](Regs& g, int step) {
-        const int ra = step * BKS + arow < n_here ? step * BKS + arow : n_here - 1;
-        g.a = *reinterpret_cast<const uint4*>(a0 + ra * ldq);
-        g.e = e0[ra * lde];
+    // The rows of a step as buffers: rows past the slab's end are read as zeros, and no load is conditional.
+    const char* ap = (const char*)codes + r_begin * ldq;
+    const char* ep = (const char*)steps + r_begin * lde;
+    const char* bp = (const char*)G + r_begin * ldg * ES;
+    const char* mp = MASK ? (const char*)mask + r_begin * ldm * 4 : nullptr;
+    int left = n_here;  // rows from the load cursor on
+    auto load = [&](Regs& g) {
+        const int rows = __builtin_amdgcn_readfirstlane(left >= BKS ? BKS : left > 0 ? left : 0);
+        const auto ra = rows_at(ap, rows * pq), re = rows_at(ep, rows * pe), rb = rows_at(bp, rows * pg);
 #pragma unroll
-        for (int p = 0; p < PB; ++p) {
-            const int rb = step * BKS + brow + p * (BKS / PB) < n_here ? step * BKS + brow + p * (BKS / PB) : n_here - 1;
-            const char* const b = b0 + rb * ldg * ES;
-            g.b[p][0] = *reinterpret_cast<const uint4*>(b);
-            if (!BF16) g.b[p][BF16 ? 0 : 1] = *reinterpret_cast<const uint4*>(b + (wide ? 16 : 0));
-            if (MASK) g.m[MASK ? p : 0] = m0[rb * ldm];
+        for (int p = 0; p < PA; ++p) {
+            g.a[p] = load16(ra, aoff[p]);
+            g.e[p] = __builtin_amdgcn_raw_buffer_load_b8(re, (int)eoff[p], 0, 0);
         }
-    };
-    auto store = [&](const Regs& g, int step, uint16_t* as, uint16_t* bs) {
-        const bool whole = (step + 1) * BKS <= n_here;
-        uint4 a = g.a;
-        if (!whole && step * BKS + arow >= n_here) a = make_uint4(0u, 0u, 0u, 0u);
-        const float unit = step_of(g.e);
-        const uint2 d0 = decode4(a.x, unit), d1 = decode4(a.y, unit), d2 = decode4(a.z, unit), d3 = decode4(a.w, unit);
-        uint16_t* const q = as + place<128>(arow, acol);
-        lds_store16(q, make_uint4(d0.x, d0.y, d1.x, d1.y));
-        lds_store16(q + 8, make_uint4(d2.x, d2.y, d3.x, d3.y));
 #pragma unroll
         for (int p = 0; p < PB; ++p) {
-            const int r = brow + p * (BKS / PB);
-            uint32_t m = MASK ? g.m[MASK ? p : 0] >> (mb % 32) : 0xFFu;
-            if (!whole && step * BKS + r >= n_here) m = 0u;
-            uint16_t* const o = bs + place<WB>(r, bcol);
+            g.b[p][0] = load16(rb, boff[p]);
+            if (!BF16) g.b[p][BF16 ? 0 : 1] = load16(rb, boff[p] + second);
+        }
+        if (MASK) {
+            const auto rm = rows_at(mp, rows * pm);
+#pragma unroll
+            for (int p = 0; p < PB; ++p) g.m[MASK ? p : 0] = __builtin_amdgcn_raw_buffer_load_b32(rm, (int)moff[p], 0, 0);
+            mp += (int64_t)BKS * pm;
+        }
+        ap += (int64_t)BKS * pq;
+        ep += (int64_t)BKS * pe;
+        bp += (int64_t)BKS * pg;
+        left -= BKS;
+    };
+    float least = 0.f;  // of the codes that this thread has met
+    auto store = [&](const Regs& g, uint16_t* as, uint16_t* bs) {
+#pragma unroll
+        for (int p = 0; p < PA; ++p) {
+            const uint32_t w[4] = {g.a[p].x, g.a[p].y, g.a[p].z, g.a[p].w};
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                f[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4)));
+                least = fminf(least, f[i]);
+            }
+            const float unit = step_of(g.e[p]);
+            uint32_t d[8];  // pairs of bf16: the upper halves, the lower ones are zero
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                d[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1] * unit), __float_as_uint(f[2 * i] * unit), 0x07060302u);
+            uint16_t* const q = as + place<WA>(arow + p * (BKS / PA), acol);
+            lds_store16(q, make_uint4(d[0], d[1], d[2], d[3]));
+            lds_store16(q + 8, make_uint4(d[4], d[5], d[6], d[7]));
+        }
+#pragma unroll
+        for (int p = 0; p < PB; ++p) {
+            const uint32_t m = MASK ? g.m[MASK ? p : 0] >> (mb % 32) : 0u;
+            uint16_t* const o = bs + place<WB>(brow + p * (BKS / PB), bcol);
             if (BF16) {
                 const uint4 v = g.b[p][0];
                 uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                if (MASK || !whole)
+                if (MASK)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         w[i] &= ((uint32_t)((int32_t)(m << (31 - 2 * i)) >> 31) & 0xFFFFu) |
@@ -385,7 +427,7 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
             } else {
                 const uint4 v0 = g.b[p][0], v1 = g.b[p][BF16 ? 0 : 1];
                 uint32_t w[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-                if (MASK || !whole)
+                if (MASK)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) w[i] &= (uint32_t)((int32_t)(m << (31 - i)) >> 31);
                 uint32_t term[3][4];
@@ -408,9 +450,9 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     auto mma = [&](const uint16_t* as, const uint16_t* bs) {
 #pragma unroll
         for (int kc = 0; kc < BKS; kc += 16) {
-            bf16x8 a[2], b[TN][PLANES];
+            bf16x8 a[TM], b[TN][PLANES];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) a[x] = read_transposed<128>(as, (wm * 2 + x) * 32, kc, lane);
+            for (int x = 0; x < TM; ++x) a[x] = read_transposed<WA>(as, (wm * TM + x) * 32, kc, lane);
 #pragma unroll
             for (int y = 0; y < TN; ++y)
 #pragma unroll
@@ -419,7 +461,7 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
 #pragma unroll
             for (int p = PLANES - 1; p >= 0; --p)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < TM; ++x)
 #pragma unroll
                     for (int y = 0; y < TN; ++y)
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[y][p], acc[x][y], 0, 0, 0);
@@ -427,64 +469,91 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     };
     if (nk > 0) {
         Regs g0, g1;
-        load(g0, 0);
-        load(g1, 1);
-        store(g0, 0, As[0], Bs[0]);
-        load(g0, 2);
+        load(g0);
+        load(g1);
+        store(g0, As[0], Bs[0]);
+        load(g0);
         __syncthreads();
         for (int i = 0; i + 1 < nk; i += 2) {
-            store(g1, i + 1, As[1], Bs[1]);
-            load(g1, i + 3);
+            store(g1, As[1], Bs[1]);
+            load(g1);
             mma(As[0], Bs[0]);
             __syncthreads();
-            store(g0, i + 2, As[0], Bs[0]);
-            load(g0, i + 4);
+            store(g0, As[0], Bs[0]);
+            load(g0);
             mma(As[1], Bs[1]);
             __syncthreads();
         }
         if (nk & 1) mma(As[0], Bs[0]);
     }
+    // Columns of Z8 that have a code -128 are NaN throughout.  It was taken for a number above; which columns they are is
+    // looked up only where one was met.
+    uint8_t* const not_finite = reinterpret_cast<uint8_t*>(As[0]);
+    __syncthreads();
+    if (tid < WA) not_finite[tid] = 0;
+    __syncthreads();
+    if (__builtin_expect(least == -128.f, 0))
+        for (int64_t r = r_begin + arow; r < r_end; r += BKS / PA)
+            for (int i = 0; i < 16; ++i)
+                if (codes[r * ldq + ka + i] == -128) not_finite[acol + i] = 1;
+    __syncthreads();
 
     // D layout: lane l, register v -> row 8 (v / 4) + 4 (l / 32) + v % 4, col l % 32
     const int li = lane & 31, lk = lane >> 5;
-    float* const out = P + (size_t)slab * KD * MD;
+    const int iw = wm * TM * 32 + 4 * lk, jw = j0 + wn * TN * 32 + li;
+    float* const out = P + ((size_t)slab * KD + i0) * MD;
     const float unscale = BF16 ? 1.f : 1.f / kTermScale;
+    float wild = 0.f;  // NaN after a sum that is not finite
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TM; ++x)
 #pragma unroll
-        for (int y = 0; y < TN; ++y) {
-            const int j = j0 + (wn * TN + y) * 32 + li;
+        for (int y = 0; y < TN; ++y)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int i = i0 + (wm * 2 + x) * 32 + 8 * (v / 4) + 4 * lk + (v % 4);
-                if (i >= KD || j >= MD) continue;
-                float sum = acc[x][y][v] * unscale;
-                if (!BF16 && __builtin_expect(!(fabsf(sum) <= 3.402823466e38f), 0)) {
-                    // Not finite: again as a chain of fp32 multiply-adds (a term of an infinity is NaN).
-                    sum = 0.f;
-                    for (int64_t r = r_begin; r < r_end; ++r) {
-                        const float z = value_of(codes[r * ldq + i], step_of(steps[r * lde + i / kGroup]));
-                        const float b = reinterpret_cast<const float*>(G)[r * ldg + j];
-                        const bool on = !MASK || ((mask[r * ldm + j / 32] >> (j % 32)) & 1u);
-                        sum = fmaf(z, on ? b : 0.f, sum);
-                    }
-                }
+                const int i = iw + x * 32 + 8 * (v / 4) + (v % 4), j = jw + y * 32;
+                if (i0 + i >= KD || j >= MD) continue;
+                const float sum = not_finite[i] ? __uint_as_float(0x7FC00000u) : acc[x][y][v] * unscale;
+                if (!BF16 && !not_finite[i]) wild = fmaf(sum, 0.f, wild);
                 out[(size_t)i * MD + j] = sum;
             }
+    if (!BF16 && __builtin_expect(!(wild == 0.f), 0)) {
+        // The lane's sums that are not finite again, as chains of fp32 multiply-adds (a term of an infinity is NaN).
+        for (int c = 0; c < TM * TN * 16; ++c) {
+            const int v = c % 16, i = iw + c / (16 * TN) * 32 + 8 * (v / 4) + (v % 4), j = jw + c / 16 % TN * 32;
+            if (i0 + i >= KD || j >= MD || not_finite[i]) continue;
+            if (fabsf(out[(size_t)i * MD + j]) <= 3.402823466e38f) continue;
+            float sum = 0.f;
+            for (int64_t r = r_begin; r < r_end; ++r) {
+                const float z = value_of(codes[r * ldq + i0 + i], step_of(steps[r * lde + (i0 + i) / kGroup]));
+                const float b = reinterpret_cast<const float*>(G)[r * ldg + j];
+                const bool on = !MASK || ((mask[r * ldm + j / 32] >> (j % 32)) & 1u);
+                sum = fmaf(z, on ? b : 0.f, sum);
+            }
+            out[(size_t)i * MD + j] = sum;
         }
+    }
 }
 
 struct Slabs {
     int64_t n, rows;
-    int nit, njt, width;
+    int nit, njt, wa, wb;  // tiles and their widths
 };
 Slabs plan_slabs(int64_t n, int32_t k, int32_t m)
 {
     Slabs s;
-    s.nit = (int)ceil_div(k, 128);
-    s.width = m > 64 ? 128 : 64;
-    s.njt = (int)ceil_div(m, s.width);
-    s.n = wgrad_slabs(n, (int64_t)s.nit * s.njt, 1024);
+    // 256 columns of Z8 where they cover no more than tiles of 128 would: what a workgroup does to its part of G, the terms
+    // and the mask, is then done for twice the cells
+    s.wa = ceil_div(k, 128) % 2 ? 128 : 256;
+    s.wb = m > 64 ? 128 : 64;
+    s.nit = (int)ceil_div(k, s.wa);
+    s.njt = (int)ceil_div(m, s.wb);
+    // two workgroups for every compute unit, of 128 rows at least (more of them and the slabs' sums cost more than they
+    // gain); four where a slab would have more than 2^14 rows, whose sums are less exact
+    const int64_t tiles = (int64_t)s.nit * s.njt;
+    s.n = ceil_div(512, tiles);
+    if (ceil_div(n, s.n) > 1 << 14) s.n = ceil_div(1024, tiles);
+    if (s.n > ceil_div(n, 128)) s.n = ceil_div(n, 128);
+    if (s.n < 1) s.n = 1;
     s.rows = ceil_div(ceil_div(n, s.n), BKS) * BKS;
     if (s.rows < BKS) s.rows = BKS;
     s.n = n > 0 ? ceil_div(n, s.rows) : 1;  // without rows: one slab of zeros
@@ -538,17 +607,22 @@ int launch_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ldq, const u
                             const void* G, int64_t ldg, float* dW, int64_t ldw, int64_t n, int32_t k, int32_t m,
                             const uint32_t* mask, int64_t ldm, float beta, float* P, hipStream_t s)
 {
+    // the rows of a step are addressed with 31 bits
+    const int64_t most = ((int64_t)1 << 31) / BKS;
+    if (n > 0 && (ldq >= most || lde >= most || ldg * (dtype == MIXGCN_BF16 ? 2 : 4) >= most || (mask && ldm * 4 >= most)))
+        return fail(MIXGCN_EUNSUPPORTED, "checkpoint_wgrad: rows of 2^26 bytes and more");
     const Slabs p = plan_slabs(n, k, m);
     const int64_t grid = p.n * p.nit * p.njt;
     if (grid > 0x7FFFFFFF || p.rows > (1 << 30)) return fail(MIXGCN_EUNSUPPORTED, "checkpoint_wgrad: too many tiles or rows");
-#define MIXGCN_WGRAD8(BF16, MASK)                                                                                         \
-    do {                                                                                                                  \
-        if (p.width == 128)                                                                                               \
-            hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK, 2>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, \
-                               ldq, steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt);                     \
-        else                                                                                                              \
-            hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK, 1>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, \
-                               ldq, steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt);                     \
+#define MIXGCN_WGRAD8_T(BF16, MASK, TM, TN)                                                                               \
+    hipLaunchKernelGGL((wgrad_checkpoint_kernel<BF16, MASK, TM, TN>), dim3((unsigned)grid), dim3(kBlock), 0, s, codes, ldq, \
+                       steps, lde, G, ldg, mask, ldm, P, k, m, p.rows, n, p.nit, p.njt)
+#define MIXGCN_WGRAD8(BF16, MASK)                                         \
+    do {                                                                  \
+        if (p.wa == 256 && p.wb == 128) MIXGCN_WGRAD8_T(BF16, MASK, 4, 2); \
+        else if (p.wa == 256) MIXGCN_WGRAD8_T(BF16, MASK, 4, 1);          \
+        else if (p.wb == 128) MIXGCN_WGRAD8_T(BF16, MASK, 2, 2);          \
+        else MIXGCN_WGRAD8_T(BF16, MASK, 2, 1);                           \
     } while (0)
     if (dtype == MIXGCN_BF16) {
         if (mask) MIXGCN_WGRAD8(true, true);
@@ -558,6 +632,7 @@ int launch_checkpoint_wgrad(int dtype, const int8_t* codes, int64_t ldq, const u
         else MIXGCN_WGRAD8(false, false);
     }
 #undef MIXGCN_WGRAD8
+#undef MIXGCN_WGRAD8_T
     MIXGCN_TRY(launch_wgrad_reduce(P, p.n, (int64_t)k * m, m, dW, ldw, beta, s));
     MIXGCN_HIP_TRY(hipGetLastError());
     return MIXGCN_OK;
