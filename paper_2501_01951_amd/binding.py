@@ -539,43 +539,52 @@ def softmax_xent(logits, labels, dlogits, loss, stream=None) -> None:
                                               _stream(stream)), "softmax_xent")
 
 
-class _on:
-    """The device of a call's tensors made current where it is not, and its stream, with which the call's
-    workspace is allocated (so that it is given back in that stream's order, and belongs to a graph that
-    is being captured there).  All tensors of a call are on one device."""
+def _one_device(*tensors) -> int:
+    """Index of the GPU that all of a call's tensors (or None) are on."""
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        raise ValueError("tensors on a GPU expected")
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    return dev.index
 
-    def __init__(self, stream, *tensors):
-        self.device = tensors[0].device
-        for t in tensors:
-            if t is not None and t.device != self.device:
-                raise ValueError(f"tensors on {self.device} and {t.device}")
-        if self.device.type != "cuda":
-            raise ValueError("tensors on a GPU expected")
-        # a stream belongs to its device: entering its context makes both current
-        self._ctx = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(self.device)
 
-    def __enter__(self):
-        self._ctx.__enter__()
-        return self
+def _issue(stream, device: int, call) -> None:
+    """call(raw stream) with the device of its tensors current, and its stream: the workspace that the call
+    allocates is then given back in that stream's order, and belongs to a graph that is being captured there."""
+    if stream is None and device == torch.cuda.current_device():
+        call(torch._C._cuda_getCurrentRawStream(device))
+        return
+    if stream is not None and stream.device.index != device:
+        raise ValueError(f"a stream of {stream.device} for tensors on cuda:{device}")
+    with torch.cuda.device(device):
+        if stream is None:
+            call(torch._C._cuda_getCurrentRawStream(device))
+        else:
+            with torch.cuda.stream(stream):
+                call(stream.cuda_stream)
 
-    def __exit__(self, *exc):
-        return self._ctx.__exit__(*exc)
 
-    def workspace(self, given, need: int):
-        if given is None:
-            return torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
-        if given.device != self.device or not given.is_contiguous():
-            raise ValueError("workspace: a contiguous tensor on the device of the others expected")
-        return given
+def _workspace(given, need: int, device: int):
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if given.device.index != device or not given.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the device of the others expected")
+    return given
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _nbytes(t) -> int:
     return t.numel() * t.element_size()
 
 
-def _shape(what: str, t, *shape, dtype=None) -> None:
-    if t is not None and (tuple(t.shape) != shape or (dtype is not None and t.dtype != dtype)):
-        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, expected {shape}" + (f" {dtype}" if dtype else ""))
+def _shape(what: str, t, shape, dtype) -> None:
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, expected {shape} {dtype}")
 
 
 def linear_xent_workspace(dtype, n: int, k: int, n_classes: int, gradients: bool = True) -> int:
@@ -591,21 +600,27 @@ def linear_xent(H, W, labels, loss=None, dH=None, dW=None, row_loss=None, worksp
     memory of linear_xent_workspace bytes to use instead of allocating it."""
     n, k = H.shape
     c = W.shape[1]
-    _shape("W", W, k, c, dtype=torch.float32)
-    _shape("labels", labels, n, dtype=torch.int32)
-    _shape("loss", loss, 1, dtype=torch.float64)
-    _shape("row_loss", row_loss, n, dtype=torch.float32)
-    _shape("dH", dH, n, k, dtype=H.dtype)
-    _shape("dW", dW, k, c, dtype=torch.float32)
-    for t in (labels, row_loss):
-        if t is not None and not t.is_contiguous():
-            raise ValueError("labels and row_loss: contiguous tensors expected")
-    with _on(stream, H, W, labels, loss, dH, dW, row_loss) as on:
-        ws = on.workspace(workspace, linear_xent_workspace(H.dtype, n, k, c, dH is not None or dW is not None))
-        _check(load_library().mixgcn_linear_xent(
-            _dtype_of(H), _ptr(H), _ld(H), _ptr(W), _ld(W), _ptr(labels), n, k, c, _ptr(loss), _ptr(row_loss), _ptr(dH),
-            _ld(dH) if dH is not None else 0, _ptr(dW), _ld(dW) if dW is not None else 0, _ptr(ws), _nbytes(ws),
-            _stream(stream)), "linear_xent")
+    dtype = _dtype_of(H)
+    _shape("W", W, (k, c), torch.float32)
+    _shape("labels", labels, (n,), torch.int32)
+    _shape("loss", loss, (1,), torch.float64)
+    _shape("row_loss", row_loss, (n,), torch.float32)
+    _shape("dH", dH, (n, k), H.dtype)
+    _shape("dW", dW, (k, c), torch.float32)
+    if not labels.is_contiguous() or (row_loss is not None and not row_loss.is_contiguous()):
+        raise ValueError("labels and row_loss: contiguous tensors expected")
+    device = _one_device(H, W, labels, loss, dH, dW, row_loss)
+    lib = load_library()
+
+    def call(raw):
+        need = lib.mixgcn_linear_xent_workspace(dtype, n, k, c, dH is not None or dW is not None)
+        ws = _workspace(workspace, max(need, 0), device)
+        _check(lib.mixgcn_linear_xent(
+            dtype, H.data_ptr(), _ld(H), W.data_ptr(), _ld(W), labels.data_ptr(), n, k, c, _address(loss),
+            _address(row_loss), _address(dH), 0 if dH is None else _ld(dH), _address(dW), 0 if dW is None else _ld(dW),
+            ws.data_ptr(), _nbytes(ws), raw), "linear_xent")
+
+    _issue(stream, device, call)
 
 
 class Checkpoint:
@@ -616,7 +631,7 @@ class Checkpoint:
         if codes.dim() != 2 or codes.dtype != torch.int8:
             raise ValueError("codes: int8 [n, cols] expected")
         n, cols = codes.shape
-        _shape("exponents", exponents, n, (cols + 31) // 32, dtype=torch.uint8)
+        _shape("exponents", exponents, (n, (cols + 31) // 32), torch.uint8)
         self.codes, self.exponents = codes, exponents
 
     @classmethod
@@ -632,24 +647,39 @@ class Checkpoint:
 def checkpoint_pack(X, kept: Checkpoint = None, stream=None) -> Checkpoint:
     """X to 8 bits."""
     n, cols = X.shape
-    with _on(stream, X, *((kept.codes, kept.exponents) if kept is not None else ())):
-        if kept is None:
-            kept = Checkpoint.empty(n, cols, X.device)
-        _shape("codes", kept.codes, n, cols)
+    dtype = _dtype_of(X)
+    if kept is not None:
+        _shape("codes", kept.codes, (n, cols), torch.int8)
+        device = _one_device(X, kept.codes, kept.exponents)
+    else:
+        device = _one_device(X)
+    made = kept
+
+    def call(raw):
+        nonlocal made
+        if made is None:
+            made = Checkpoint.empty(n, cols, X.device)
         _check(load_library().mixgcn_checkpoint_pack(
-            _dtype_of(X), _ptr(X), _ld(X), n, cols, _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents),
-            _ld(kept.exponents), _stream(stream)), "checkpoint_pack")
-    return kept
+            dtype, X.data_ptr(), _ld(X), n, cols, made.codes.data_ptr(), _ld(made.codes), made.exponents.data_ptr(),
+            _ld(made.exponents), raw), "checkpoint_pack")
+
+    _issue(stream, device, call)
+    return made
 
 
 def checkpoint_unpack(kept: Checkpoint, X, stream=None) -> None:
     """The values of a checkpoint into X (n x cols, float32 or bfloat16)."""
-    n, cols = kept.shape
-    _shape("X", X, n, cols)
-    with _on(stream, X, kept.codes, kept.exponents):
+    codes, exponents = kept.codes, kept.exponents
+    n, cols = codes.shape
+    dtype = _dtype_of(X)
+    _shape("X", X, (n, cols), X.dtype)
+
+    def call(raw):
         _check(load_library().mixgcn_checkpoint_unpack(
-            _dtype_of(X), _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents), _ld(kept.exponents), n, cols, _ptr(X),
-            _ld(X), _stream(stream)), "checkpoint_unpack")
+            dtype, codes.data_ptr(), _ld(codes), exponents.data_ptr(), _ld(exponents), n, cols, X.data_ptr(), _ld(X),
+            raw), "checkpoint_unpack")
+
+    _issue(stream, _one_device(X, codes, exponents), call)
 
 
 def checkpoint_wgrad_workspace(n: int, k: int, m: int) -> int:
@@ -659,16 +689,23 @@ def checkpoint_wgrad_workspace(n: int, k: int, m: int) -> int:
 
 def checkpoint_wgrad(kept: Checkpoint, G, dW, mask=None, beta: float = 0.0, workspace=None, stream=None) -> None:
     """dW = beta dW + Z^T (G (.) M) with Z the values of a checkpoint; mask: bitmap of G's shape (relu_bitmap)."""
-    n, k = kept.shape
+    codes, exponents = kept.codes, kept.exponents
+    n, k = codes.shape
     m = G.shape[1]
-    _shape("G", G, n, m)
-    _shape("dW", dW, k, m, dtype=torch.float32)
+    dtype = _dtype_of(G)
+    _shape("G", G, (n, m), G.dtype)
+    _shape("dW", dW, (k, m), torch.float32)
     if mask is not None and (mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2 or mask.shape[0] != n or
                              mask.shape[1] < (m + 31) // 32 or mask.stride(1) != 1):
         raise ValueError("mask: int32 [n, ceil(m / 32)] expected")
-    with _on(stream, G, kept.codes, kept.exponents, dW, mask) as on:
-        ws = on.workspace(workspace, checkpoint_wgrad_workspace(n, k, m))
-        _check(load_library().mixgcn_checkpoint_wgrad(
-            _dtype_of(G), _ptr(kept.codes), _ld(kept.codes), _ptr(kept.exponents), _ld(kept.exponents), _ptr(G), _ld(G),
-            _ptr(dW), _ld(dW), n, k, m, _ptr(mask), mask.stride(0) if mask is not None else 0, beta, _ptr(ws), _nbytes(ws),
-            _stream(stream)), "checkpoint_wgrad")
+    device = _one_device(G, codes, exponents, dW, mask)
+    lib = load_library()
+
+    def call(raw):
+        ws = _workspace(workspace, max(lib.mixgcn_checkpoint_wgrad_workspace(n, k, m), 0), device)
+        _check(lib.mixgcn_checkpoint_wgrad(
+            dtype, codes.data_ptr(), _ld(codes), exponents.data_ptr(), _ld(exponents), G.data_ptr(), _ld(G), dW.data_ptr(),
+            _ld(dW), n, k, m, _address(mask), 0 if mask is None else mask.stride(0), beta, ws.data_ptr(), _nbytes(ws),
+            raw), "checkpoint_wgrad")
+
+    _issue(stream, device, call)
