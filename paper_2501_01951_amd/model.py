@@ -286,3 +286,76 @@ class GCNDropoutStep:
     def step(self):
         self.forward()
         self.backward()
+
+
+class GCNCheckpointStep:
+    """GCNStep in the order of Algorithm 2 that keeps little for its backward pass, for graphs whose activations
+    and logits do not fit: of a hidden layer the aggregate Z_l in 8 bits and the ReLU derivative as bits, and of the
+    last layer nothing, whose loss and gradients come from Z and W without logits (linear_xent).  Per node and layer
+    that is f_in (1 + 1/32) + f_out / 8 bytes instead of 4 (f_in + f_out) (fp32); Z, H and their gradients
+    take one pair of n x f buffers per width.  The forward products and the input gradients are those of the
+    full-precision step; the hidden layers' weight gradients are of the 8-bit aggregates.
+
+    labels: int32 [n]; a node whose label is not a class has none and takes no part in the loss.
+    For few classes GCNStep, which multiplies by a narrowing W before it aggregates, is the faster one."""
+
+    def __init__(self, g: B.Graph, x, weights, labels):
+        self.g, self.n, self.labels = g, x.shape[0], labels
+        self.w = list(weights)
+        dev, dt = x.device, x.dtype
+        self.x = padded_rows(self.n, x.shape[1], dt, dev)
+        self.x.copy_(x)
+        L = len(self.w)
+        widths = {w.shape[0] for w in self.w}
+        # a layer's input is dead once it is aggregated, its aggregate once it is packed and multiplied: one buffer of
+        # either per width serves all layers, and their gradients on the way back
+        self.z = {f: padded_rows(self.n, f, dt, dev) for f in widths}
+        self.h = {f: padded_rows(self.n, f, dt, dev) for f in widths}
+        self.kept = [B.Checkpoint.empty(self.n, w.shape[0], dev) for w in self.w[:L - 1]]
+        self.positive = [torch.empty(self.n, (w.shape[1] + 31) // 32, dtype=torch.int32, device=dev) for w in self.w[:L - 1]]
+        self.dw = [torch.empty_strided(w.shape, w.stride(), dtype=w.dtype, device=dev) for w in self.w]
+        self.loss = torch.zeros(1, dtype=torch.float64, device=dev)
+        need = [B.linear_xent_workspace(dt, self.n, *self.w[-1].shape)]
+        need += [B.checkpoint_wgrad_workspace(self.n, *w.shape) for w in self.w[:L - 1]]
+        self.workspace = torch.empty(max(need), dtype=torch.uint8, device=dev)
+
+    def _aggregates(self, keep: bool):
+        """The last layer's aggregate; with `keep`, the others' go into their checkpoints."""
+        h = self.x
+        for l, w in enumerate(self.w):
+            k, m = w.shape
+            B.aggregate(self.g, h, self.z[k])
+            if l == len(self.w) - 1:
+                return self.z[k]
+            if keep:
+                B.checkpoint_pack(self.z[k], self.kept[l])
+            h = self.h[m]
+            B.update(B.OP_FWD_RELU, self.z[k], w, h, self.n, k, m)
+            if keep:
+                B.relu_bitmap(h, self.positive[l])
+
+    def forward(self):
+        """Loss, and the last layer's gradients: of its weights into dw, of its aggregate over the aggregate."""
+        z = self._aggregates(True)
+        B.linear_xent(z, self.w[-1], self.labels, loss=self.loss, dH=z if len(self.w) > 1 else None, dW=self.dw[-1],
+                      workspace=self.workspace)
+
+    def backward(self):
+        for l in range(len(self.w) - 2, -1, -1):
+            k, m = self.w[l].shape
+            # dZ of the layer above through A_hat^T, times this layer's ReLU derivative
+            B.aggregate_masked(self.g, self.z[m], self.h[m], self.positive[l], transpose=True)
+            B.checkpoint_wgrad(self.kept[l], self.h[m], self.dw[l], workspace=self.workspace)
+            if l > 0:
+                B.update(B.OP_DGRAD, self.h[m], self.w[l], self.z[k], self.n, k, m)
+
+    def step(self):
+        self.forward()
+        self.backward()
+
+    def score(self, labels=None, out=None):
+        """Loss of every node (float32 [n], 0 without a label) with the present weights, for validation."""
+        labels = self.labels if labels is None else labels
+        out = torch.empty(self.n, device=self.x.device) if out is None else out
+        B.linear_xent(self._aggregates(False), self.w[-1], labels, row_loss=out, workspace=self.workspace)
+        return out
