@@ -416,7 +416,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 // before which a wavefront waits for its own part of the step that is due and for what it has read.  LDS holds rows
 // without padding, so the 16-byte pieces of a row are put in another order, which each lane fetches from: rows of 64
 // bytes have piece p at p ^ (row / 4 % 4), and rows of the free index, in which the transposing read takes 64 bytes of
-// four rows at a time, the 64-byte block q at q ^ (row % 4).  Either way the lanes that are served together hit all
+// four rows at a time, the 64-byte block q at q ^ (row % 4) (of rows of two blocks q ^ (row / 2 % 2)).  Either way the lanes that are served together hit all
 // banks.
 struct Operand {
     const uint16_t* p;  // first term of the tile's first element
@@ -449,13 +449,20 @@ struct Product {
     static constexpr int IA = PA / 512 / 4, IB = PB / 512 / 4;    // loads of a wavefront per plane
     static constexpr int LOADS = TA * IA + TB * IB;
 
+    // what the 64-byte block of a row of the reduction index is exclusive-ored with
+    template <int WIDTH>
+    static __device__ inline int turn(int row)
+    {
+        static_assert(WIDTH >= 64, "two blocks to a row at least");
+        return WIDTH == 64 ? row >> 1 & 1 : row & 3;
+    }
     // where lane `lane` of load `i` of a plane reads, in bytes from the plane's first element of the step
     template <bool TR, int WIDTH>
     static __device__ inline uint32_t source(int64_t rows, int i, int lane)
     {
         if (TR) {
             const int row = (i * 64 + lane) / (WIDTH / 8), slot = (i * 64 + lane) % (WIDTH / 8);
-            return (uint32_t)((slot / 4 ^ (row & 3)) * rows * 64) + 64u * (uint32_t)row + 16u * (uint32_t)(slot % 4);
+            return (uint32_t)((slot / 4 ^ turn<WIDTH>(row)) * rows * 64) + 64u * (uint32_t)row + 16u * (uint32_t)(slot % 4);
         }
         const int row = i * 16 + lane / 4, slot = lane % 4;
         return 64u * (uint32_t)row + 16u * (uint32_t)(slot ^ ((row >> 2) & 3));
@@ -467,7 +474,7 @@ struct Product {
         half8 o;
         if (TR) {
             const int grp = lane >> 4, gs = lane & 15, row = kc + 8 * (grp >> 1) + (gs >> 2);
-            const uint16_t* const p = t + row * WIDTH + (((free0 / 32) ^ (row & 3)) * 32) + 16 * (grp & 1) + 4 * (gs & 3);
+            const uint16_t* const p = t + row * WIDTH + ((free0 / 32 ^ turn<WIDTH>(row)) * 32) + 16 * (grp & 1) + 4 * (gs & 3);
             const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)p);
             const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * WIDTH));
             const shortx8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -655,13 +662,13 @@ __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* _
 }
 
 // A row's largest t and what its exponentials are taken times for G, from the sums of its pieces; the loss of the row.
-// A block takes ROWS rows, kBlock / ROWS lanes walk the pieces of each.
+// A block takes ROWS rows, kBlock / ROWS lanes walk the pieces of each; losses[block]: the sum of its rows' losses.
 template <int ROWS>
 __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restrict__ sums, int pieces,
                                                            const float* __restrict__ at_label,
                                                            const Meta* __restrict__ meta, uint32_t first, int piece_rows,
                                                            const uint32_t* __restrict__ rows, float2* __restrict__ norm,
-                                                           float* __restrict__ losses, float* __restrict__ row_loss)
+                                                           double* __restrict__ losses, float* __restrict__ row_loss)
 {
     constexpr int LANES = kBlock / ROWS;
     __shared__ float tops[LANES][ROWS + 1], parts[LANES][ROWS + 1];
@@ -694,6 +701,7 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
     tops[q][j] = top;
     parts[q][j] = bad ? __uint_as_float(0x7FC00000u) : sum;
     __syncthreads();
+    float l = 0.f;
     if (q == 0 && row < live) {
         float m = -INFINITY;
         for (int i = 0; i < LANES; ++i) m = fmaxf(m, tops[i][j]);
@@ -703,35 +711,43 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
             s += parts[i][j] * (tops[i][j] > -INFINITY ? __builtin_amdgcn_exp2f(tops[i][j] - m) : 0.f);
         if (!(m > -INFINITY)) s = __uint_as_float(0x7FC00000u);
         norm[row] = make_float2(m, kGradScale / s);
-        const float l = ((m - at_label[row]) + log2f(s)) * kLn2;
-        losses[first + row] = l;
+        l = ((m - at_label[row]) + log2f(s)) * kLn2;
         if (row_loss) row_loss[rows[first + row]] = l;
+    }
+    __syncthreads();
+    if (q == 0) parts[0][j] = l;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double sum = 0.0;
+        for (int i = 0; i < ROWS; ++i) sum += (double)parts[0][i];
+        losses[first / ROWS + blockIdx.x] = sum;
     }
 }
 
-// Mean of the losses in a fixed order; 0 without rows.
-__global__ __launch_bounds__(1024) void mean_loss_kernel(const float* __restrict__ losses, const Meta* __restrict__ meta,
-                                                         double* __restrict__ loss)
+// Mean of the losses, from the sums of `per` rows each, in a fixed order; 0 without rows.
+__device__ inline void mean_loss(const double* __restrict__ losses, int per, uint32_t count, double* __restrict__ loss)
 {
-    __shared__ double sh[1024 / kWave];
-    const int64_t count = meta->count;
+    __shared__ double sh[kBlock / kWave];
+    const int64_t parts = ((int64_t)count + per - 1) / per;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < count; i += 8 * 1024) {
-        float v[8];
+    for (int64_t i = threadIdx.x; i < parts; i += 8 * kBlock) {
+        double v[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = i + u * 1024 < count ? losses[i + u * 1024] : 0.f;
+        for (int u = 0; u < 8; ++u) v[u] = i + u * kBlock < parts ? losses[i + u * kBlock] : 0.0;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += (double)v[u];
+        for (int u = 0; u < 8; ++u) s += v[u];
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        s = 0.0;
-        for (int w = 0; w < 1024 / kWave; ++w) s += sh[w];
-        *loss = count ? s / (double)count : 0.0;
-    }
+    if (threadIdx.x == 0) *loss = count ? ((sh[0] + sh[1]) + (sh[2] + sh[3])) / (double)count : 0.0;
+}
+
+__global__ __launch_bounds__(kBlock) void mean_loss_kernel(const double* __restrict__ losses, int per,
+                                                           const Meta* __restrict__ meta, double* __restrict__ loss)
+{
+    mean_loss(losses, per, meta->count, loss);
 }
 
 // ---- gradient with respect to the logits --------------------------------------------------------
@@ -804,60 +820,113 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
     }
 }
 
-// ---- dH -----------------------------------------------------------------------------------------
-// part[slab][row][kp] (+)= G[row][classes of the slab] W'^T.  One term each (bf16 features, whose gradient is rounded
-// to 8 bits afterwards) or two.
-template <int T>
-struct GradRows {
-    static constexpr int TM = T == 1 ? 4 : 2, TN = 2, STAGES = T == 1 ? 3 : 2;
-    using P = Product<T, T, false, true, TM, TN, STAGES>;
-    static constexpr int ROWS = 64 * TM;
+// ---- dH and dW ----------------------------------------------------------------------------------
+// Of a block of G (the listed rows from `first` on, the classes from col0 on):
+//   dh[slab][row][kp] (+)= G[row][classes of the slab] W'^T,     dw[slab][kp][piece_cols] = H'^T[rows of the slab] G.
+// One launch has the workgroups of both, row_blocks of dH first.
+struct Gradients {
+    const uint16_t *g, *hp, *wp;
+    int kp, h_rows, w_rows, g_rows;
+    const Meta* meta;
+    uint32_t first;
+    int piece_rows, piece_cols, col0;
+    int row_blocks, row_slabs, row_slab_cols;  // dH: its classes are dealt to slabs
+    bool add;
+    float* dh;
+    int w_slabs;                               // dW: its rows are dealt to slabs
+    float* dw;
 };
 
-template <int T>
-__global__ __launch_bounds__(kBlock, 2) void grad_rows_kernel(const uint16_t* __restrict__ Gp, int g_rows, int piece_cols,
-                                                              int piece_rows, const uint16_t* __restrict__ Wp, int kp,
-                                                              int w_rows, int col0,
-                                                              const Meta* __restrict__ meta, uint32_t first, int slab_cols,
-                                                              int k_tiles, int slabs, bool add, float* __restrict__ part)
-{
-    using S = GradRows<T>;
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[S::P::LDS];
-    const unsigned row_tiles = (unsigned)(rows_here(meta, first, piece_rows) + S::ROWS - 1) / S::ROWS;
-    const unsigned tiles = row_tiles * (unsigned)(k_tiles * slabs);
-    if (blockIdx.x >= tiles) return;
-    const unsigned lid = xcd_local_index(blockIdx.x, tiles);
-    const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
-    const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % slabs));
-    const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * slabs)) * S::ROWS);
-    const int s0 = slab * slab_cols;
-    const int s1 = s0 + slab_cols < piece_cols ? s0 + slab_cols : piece_cols;
-    if (add && s1 <= s0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-    floatx16 acc[S::TM][S::TN];
-    clear(acc);
-    S::P::run({Gp + ((size_t)(s0 / BK) * g_rows + r0) * BK, g_rows, (size_t)piece_cols * g_rows},
-              {Wp + ((size_t)(kt * kTile / BK) * w_rows + col0 + s0) * BK, w_rows, (size_t)kp * w_rows}, s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
-    float* const out = part + ((size_t)slab * piece_rows + r0 + wm * S::TM * 32) * kp + kt * kTile + wn * 64 + (lane & 31);
+// Tiles of 64 TM rows x 64 TN features.  One term each (bf16 features, whose gradient is rounded to 8 bits afterwards) or two.
+template <int T, int TN>
+struct GradRows {
+    static constexpr int TM = T == 1 ? 4 : 2, STAGES = T == 1 ? 3 : 2;
+    using P = Product<T, T, false, true, TM, TN, STAGES>;
+    static constexpr int ROWS = 64 * TM;
+
+    static __device__ inline void run(const Gradients& a, uint16_t* lds)
+    {
+        const int k_tiles = a.kp / P::WB;
+        const unsigned row_tiles = (unsigned)(rows_here(a.meta, a.first, a.piece_rows) + ROWS - 1) / ROWS;
+        const unsigned tiles = row_tiles * (unsigned)(k_tiles * a.row_slabs);
+        if (blockIdx.x >= tiles) return;
+        const unsigned lid = xcd_local_index(blockIdx.x, tiles);
+        const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
+        const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % a.row_slabs));
+        const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * a.row_slabs)) * ROWS);
+        const int s0 = slab * a.row_slab_cols;
+        const int s1 = s0 + a.row_slab_cols < a.piece_cols ? s0 + a.row_slab_cols : a.piece_cols;
+        if (a.add && s1 <= s0) return;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+        floatx16 acc[TM][TN];
+        clear(acc);
+        P::run({a.g + ((size_t)(s0 / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
+               {a.wp + ((size_t)(kt * P::WB / BK) * a.w_rows + a.col0 + s0) * BK, a.w_rows, (size_t)a.kp * a.w_rows},
+               s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
+        float* const out =
+            a.dh + ((size_t)slab * a.piece_rows + r0 + wm * TM * 32) * a.kp + kt * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
-    for (int x = 0; x < S::TM; ++x) {
-        if (add) {
-            // all loads of a row of tiles before its first store (left to follow each other they cost 56 us a piece)
-            float had[S::TN][16];
+        for (int x = 0; x < TM; ++x) {
+            if (a.add) {
+                // all loads of a row of tiles before its first store (left to follow each other they cost 56 us a piece)
+                float had[TN][16];
 #pragma unroll
-            for (int y = 0; y < S::TN; ++y)
+                for (int y = 0; y < TN; ++y)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) had[y][v] = out[(size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32];
+                    for (int v = 0; v < 16; ++v) had[y][v] = out[(size_t)(x * 32 + tile_row(v, lane)) * a.kp + y * 32];
 #pragma unroll
-            for (int y = 0; y < S::TN; ++y)
+                for (int y = 0; y < TN; ++y)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[x][y][v] += had[y][v];
+                    for (int v = 0; v < 16; ++v) acc[x][y][v] += had[y][v];
+            }
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) out[(size_t)(x * 32 + tile_row(v, lane)) * a.kp + y * 32] = acc[x][y][v];
         }
-#pragma unroll
-        for (int y = 0; y < S::TN; ++y)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) out[(size_t)(x * 32 + tile_row(v, lane)) * kp + y * 32] = acc[x][y][v];
     }
+};
+
+// Tiles of 64 TM features x 128 classes.
+template <int T, int TM>
+struct GradWeights {
+    using P = Product<T, 2, true, true, TM, 2, 2>;
+
+    static __device__ inline void run(const Gradients& a, uint16_t* lds)
+    {
+        const int k_tiles = a.kp / P::WA, class_tiles = a.piece_cols / kTile;
+        const unsigned lid = xcd_local_index(blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
+        const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
+        const int ct = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % class_tiles));
+        const int slab = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * class_tiles)));
+        const int live = rows_here(a.meta, a.first, a.piece_rows);
+        const int per = ((live + a.w_slabs - 1) / a.w_slabs + BK - 1) / BK * BK;
+        const int r0 = slab * per, r1 = r0 + per < live ? r0 + per : live;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+        floatx16 acc[TM][2];
+        clear(acc);
+        P::run({a.hp + ((size_t)(kt * P::WA / BK) * a.h_rows + r0) * BK, a.h_rows, (size_t)a.kp * a.h_rows},
+               {a.g + ((size_t)(ct * kTile / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
+               r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
+        float* const out = a.dw + ((size_t)slab * a.kp + kt * P::WA + wm * TM * 32) * a.piece_cols + ct * kTile + wn * 64 + (lane & 31);
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    out[(size_t)(x * 32 + tile_row(v, lane)) * a.piece_cols + y * 32] = acc[x][y][v];
+    }
+};
+
+template <int T, int TN, int TM>
+__global__ __launch_bounds__(kBlock, 2) void gradients_kernel(Gradients a)
+{
+    using R = GradRows<T, TN>;
+    using W = GradWeights<T, TM>;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[R::P::LDS > W::P::LDS ? R::P::LDS : W::P::LDS];
+    if ((int)blockIdx.x < a.row_blocks) R::run(a, lds);
+    else W::run(a, lds);
 }
 
 // The sum of four neighboring cells over the slabs, for SL lanes that share the cells: lane 0 of them has it.
@@ -894,108 +963,96 @@ __device__ inline float4 sum_slabs(const float* p, size_t slab, int slabs, bool 
     return s;
 }
 
-// dH of the listed rows from the slabs' sums.
+// What ends a block of G: dH of the listed rows from the slabs' sums (row_blocks blocks), dW[k][classes of the piece] (+)= the slabs'
+// sums (w_blocks), and the mean of the losses (one more, where loss is given).
+struct Finish {
+    const float* dh;
+    int row_blocks, row_slabs, piece_rows;
+    const uint32_t* rows;
+    void* dH;
+    int64_t ldd;
+    const float* dw;
+    int w_blocks, w_slabs, piece_cols, cols;
+    bool add;
+    float* dW;
+    int64_t ldg;
+    int k, kp;
+    const int32_t* shift;
+    const Meta* meta;
+    uint32_t first;
+    const double* losses;
+    int loss_rows;
+    double* loss;
+};
+
 template <bool BF16, int SL>
-__global__ __launch_bounds__(kBlock) void finish_rows_kernel(const float* __restrict__ part, int slabs, int piece_rows, int k,
-                                                             int kp, const int32_t* __restrict__ shift,
-                                                             const Meta* __restrict__ meta, uint32_t first,
-                                                             const uint32_t* __restrict__ rows, void* __restrict__ dH,
-                                                             int64_t ldd)
+__device__ inline void finish_rows(const Finish& a)
 {
     __shared__ float4 lds[SL][kBlock / SL];
-    const int live = rows_here(meta, first, piece_rows);
-    const int per_row = (k + 3) / 4;
-    const int64_t it = (int64_t)blockIdx.x * (kBlock / SL) + threadIdx.x % (kBlock / SL);
-    if ((int64_t)blockIdx.x * (kBlock / SL) >= (int64_t)live * per_row) return;
+    const int live = rows_here(a.meta, a.first, a.piece_rows);
+    const int per_row = (a.k + 3) / 4;
+    const int64_t it0 = (int64_t)blockIdx.x * (kBlock / SL), it = it0 + threadIdx.x % (kBlock / SL);
+    if (it0 >= (int64_t)live * per_row) return;
     const bool in = it < (int64_t)live * per_row;
     const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
-    const float4 s = sum_slabs<SL>(part + (size_t)i * kp + j, (size_t)piece_rows * kp, slabs, in, lds);
+    const float4 s = sum_slabs<SL>(a.dh + (size_t)i * a.kp + j, (size_t)a.piece_rows * a.kp, a.row_slabs, in, lds);
     if (!in || threadIdx.x >= kBlock / SL) return;
-    const float inv = 1.f / (float)meta->count;
+    const float inv = 1.f / (float)a.meta->count;
     const float v[4] = {s.x, s.y, s.z, s.w};
     float o[4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - shift[kp + j + b]);
-    const int64_t at = (int64_t)rows[first + i] * ldd + j;
+    for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - a.shift[a.kp + j + b]);
+    const int64_t at = (int64_t)a.rows[a.first + i] * a.ldd + j;
     if (BF16) {
         const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-        if (j + 4 <= k) *reinterpret_cast<uint2*>((uint16_t*)dH + at) = make_uint2(w[0], w[1]);
+        if (j + 4 <= a.k) *reinterpret_cast<uint2*>((uint16_t*)a.dH + at) = make_uint2(w[0], w[1]);
         else
-            for (int b = 0; j + b < k; ++b) ((uint16_t*)dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
+            for (int b = 0; j + b < a.k; ++b) ((uint16_t*)a.dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
     } else {
-        if (j + 4 <= k) *reinterpret_cast<float4*>((float*)dH + at) = make_float4(o[0], o[1], o[2], o[3]);
+        if (j + 4 <= a.k) *reinterpret_cast<float4*>((float*)a.dH + at) = make_float4(o[0], o[1], o[2], o[3]);
         else
-            for (int b = 0; j + b < k; ++b) ((float*)dH)[at + b] = o[b];
+            for (int b = 0; j + b < a.k; ++b) ((float*)a.dH)[at + b] = o[b];
     }
 }
 
-// ---- dW -----------------------------------------------------------------------------------------
-// part[slab][kp][piece_cols] = H'^T[rows of the slab] G.  Tiles of 64 TM features x 128 classes.
-template <int TH, int TM>
-__global__ __launch_bounds__(kBlock, 2) void grad_weights_kernel(const uint16_t* __restrict__ Hp, int kp, int h_rows,
-                                                                 const uint16_t* __restrict__ Gp, int g_rows, int piece_cols,
-                                                                 int piece_rows, const Meta* __restrict__ meta, uint32_t first,
-                                                                 int class_tiles, int k_tiles, int slabs,
-                                                                 float* __restrict__ part)
-{
-    using P = Product<TH, 2, true, true, TM, 2, 2>;
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[P::LDS];
-    const unsigned lid = xcd_local_index(blockIdx.x, gridDim.x);
-    const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
-    const int ct = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % class_tiles));
-    const int slab = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * class_tiles)));
-    const int live = rows_here(meta, first, piece_rows);
-    const int per = ((live + slabs - 1) / slabs + BK - 1) / BK * BK;
-    const int r0 = slab * per, r1 = r0 + per < live ? r0 + per : live;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-    floatx16 acc[TM][2];
-    clear(acc);
-    P::run({Hp + ((size_t)(kt * P::WA / BK) * h_rows + r0) * BK, h_rows, (size_t)kp * h_rows},
-           {Gp + ((size_t)(ct * kTile / BK) * g_rows + r0) * BK, g_rows, (size_t)piece_cols * g_rows},
-           r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
-    float* const out = part + ((size_t)slab * kp + kt * P::WA + wm * TM * 32) * piece_cols + ct * kTile + wn * 64 + (lane & 31);
-#pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                out[(size_t)(x * 32 + tile_row(v, lane)) * piece_cols + y * 32] = acc[x][y][v];
-}
-
-// dW[k][classes of the piece] (+)= the slabs' sums, unscaled.
 template <int SL>
-__global__ __launch_bounds__(kBlock) void finish_weights_kernel(const float* __restrict__ part, int slabs, int k, int kp,
-                                                                int piece_cols, int cols, const int32_t* __restrict__ shift,
-                                                                const Meta* __restrict__ meta, uint32_t first, bool add,
-                                                                float* __restrict__ dW, int64_t ldw)
+__device__ inline void finish_weights(const Finish& a)
 {
     __shared__ float4 lds[SL][kBlock / SL];
-    const uint32_t count = meta->count;
-    if (add && first >= count) return;
-    const int per_row = (cols + 3) / 4;
-    const int64_t it = (int64_t)blockIdx.x * (kBlock / SL) + threadIdx.x % (kBlock / SL);
-    const bool in = it < (int64_t)k * per_row;
+    const uint32_t count = a.meta->count;
+    if (a.add && a.first >= count) return;
+    const int per_row = (a.cols + 3) / 4;
+    const int64_t it = (int64_t)(blockIdx.x - a.row_blocks) * (kBlock / SL) + threadIdx.x % (kBlock / SL);
+    const bool in = it < (int64_t)a.k * per_row;
     const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
-    const float4 s = sum_slabs<SL>(part + (size_t)i * piece_cols + j, (size_t)kp * piece_cols, slabs, in, lds);
+    const float4 s = sum_slabs<SL>(a.dw + (size_t)i * a.piece_cols + j, (size_t)a.kp * a.piece_cols, a.w_slabs, in, lds);
     if (!in || threadIdx.x >= kBlock / SL) return;
     const float inv = count ? 1.f / (float)count : 0.f;
     const float v[4] = {s.x, s.y, s.z, s.w};
-    float* const o = dW + (int64_t)i * ldw + j;
-    const int e = -15 - shift[i];
-    if (j + 4 <= cols) {
+    float* const o = a.dW + (int64_t)i * a.ldg + j;
+    const int e = -15 - a.shift[i];
+    if (j + 4 <= a.cols) {
         float4 g = make_float4(ldexpf(v[0] * inv, e), ldexpf(v[1] * inv, e), ldexpf(v[2] * inv, e), ldexpf(v[3] * inv, e));
-        if (add) {
+        if (a.add) {
             const float4 d = *reinterpret_cast<const float4*>(o);
             g = make_float4(d.x + g.x, d.y + g.y, d.z + g.z, d.w + g.w);
         }
         *reinterpret_cast<float4*>(o) = g;
     } else {
-        for (int b = 0; j + b < cols; ++b) {
+        for (int b = 0; j + b < a.cols; ++b) {
             const float g = ldexpf(v[b] * inv, e);
-            o[b] = add ? o[b] + g : g;
+            o[b] = a.add ? o[b] + g : g;
         }
     }
+}
+
+// RL, WL: lanes that share a cell of dH and of dW, 16 where there are many slabs
+template <bool BF16, int RL, int WL>
+__global__ __launch_bounds__(kBlock) void finish_kernel(Finish a)
+{
+    if ((int)blockIdx.x < a.row_blocks) finish_rows<BF16, RL>(a);
+    else if ((int)blockIdx.x < a.row_blocks + a.w_blocks) finish_weights<WL>(a);
+    else mean_loss(a.losses, a.loss_rows, a.meta->count, a.loss);
 }
 
 // ---- plan ---------------------------------------------------------------------------------------
@@ -1006,7 +1063,9 @@ struct Layout {
     int piece_rows, piece_cols;     // a block of G
     int row_pieces, col_pieces;
     int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
-    int w_slabs, w_width;           // dW: rows of a piece dealt to slabs; features of a tile
+    int w_slabs;                    // dW: rows of a piece dealt to slabs
+    int r_width, w_width;           // features of a tile of dH, of dW
+    int loss_rows;                  // rows of a partial sum of the losses
     int list_step, list_blocks;
     size_t meta, counts, rows, top, shift, hp, wp, y, sums, at_label, norm, losses, g, dh, dw, bytes;
 };
@@ -1018,12 +1077,13 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
 {
     Layout l;
     l.terms = dtype == MIXGCN_BF16 ? 1 : 2;
-    l.kp = (int)up(k, kTile);
+    // tiles of 64 features where they are a quarter less than tiles of 128 (k up to 64, 129 to 192)
+    l.kp = (int)(4 * up(k, 64) <= 3 * up(k, 128) ? up(k, 64) : up(k, 128));
     l.cp = (int)up(c, kTile);
     // G, four bytes a logit, is handed on in blocks of 2^26 logits at most: as many classes as give dW a tile for
     // every compute unit without a split of the rows, and rows for the rest
     const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
-    int64_t cols = between(2048, up(32768 / (l.kp / kTile), kTile), 32768);
+    int64_t cols = between(2048, up((int64_t)32768 * kTile / l.kp, kTile), 32768);
     if (cols > l.cp) cols = l.cp;
     int64_t rows = between(2048, most / cols / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
     if (rows > all_rows) rows = all_rows;
@@ -1035,14 +1095,15 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.w_rows = l.cp + 2;
     l.row_pieces = (int)ceil_div(all_rows, rows);
     l.col_pieces = (int)ceil_div(l.cp, cols);
-    const int64_t k_tiles = l.kp / kTile, col_tiles = cols / kTile;
+    l.r_width = l.kp % 128 ? 64 : 128;
+    l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 ? 256 : 128;
     // two workgroups for every compute unit
-    const int64_t row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1>::ROWS : GradRows<2>::ROWS);
-    int64_t s = between(1, 512 / (k_tiles * row_tiles), col_tiles);
+    const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
+    const int64_t s = between(1, 512 / (l.kp / l.r_width * row_tiles), col_tiles);
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
-    l.w_width = l.terms == 1 && l.kp % 256 == 0 ? 256 : 128;
     l.w_slabs = (int)between(1, 512 / (l.kp / l.w_width * col_tiles), rows / kTile);
+    l.loss_rows = rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
     size_t at = 0;
@@ -1062,7 +1123,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.sums = take((size_t)(l.cp / kHalfTile) * rows * 8);
     l.at_label = take((size_t)rows * 4);
     l.norm = take((size_t)rows * 8);
-    l.losses = take((size_t)n * 4);
+    l.losses = take((size_t)(ceil_div(n, l.loss_rows) + 1) * 8);
     l.g = l.dh = l.dw = 0;
     if (gradients) {
         l.g = take((size_t)2 * l.g_rows * cols * 2);
@@ -1100,7 +1161,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     float2* const sums = (float2*)(ws + l.sums);
     float* const at_label = (float*)(ws + l.at_label);
     float2* const norm = (float2*)(ws + l.norm);
-    float* const losses = (float*)(ws + l.losses);
+    double* const losses = (double*)(ws + l.losses);
     uint16_t* const g = (uint16_t*)(ws + l.g);
     float* const dhp = (float*)(ws + l.dh);
     float* const dwp = (float*)(ws + l.dw);
@@ -1109,6 +1170,11 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     do {                                                        \
         if (bf16) MIXGCN_RUN(KERNEL<true>, GRID, __VA_ARGS__);  \
         else MIXGCN_RUN(KERNEL<false>, GRID, __VA_ARGS__);      \
+    } while (0)
+#define MIXGCN_RUN_T3(KERNEL, R, W, GRID, ...)                         \
+    do {                                                               \
+        if (bf16) MIXGCN_RUN((KERNEL<true, R, W>), GRID, __VA_ARGS__); \
+        else MIXGCN_RUN((KERNEL<false, R, W>), GRID, __VA_ARGS__);     \
     } while (0)
     if (l.list_blocks > 1) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts);
     MIXGCN_RUN(list_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, rows, meta, top, 2 * l.kp);
@@ -1120,7 +1186,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), kBlock), 4096) : 0;
     MIXGCN_RUN_T(top_kernel, tp.w_blocks + tp.h_blocks + tp.clear_blocks, H, ldh, rows, meta, W, ldw, k, c, l.kp, tp, top, labels,
                  n, dH, ldd, row_loss);
-    const int nk = (int)ceil_div(k, BK), k_tiles = l.kp / kTile, class_tiles = l.cp / kTile, pr = l.piece_rows;
+    const int nk = (int)ceil_div(k, BK), class_tiles = l.cp / kTile, pr = l.piece_rows;
     const int pieces = l.cp / kHalfTile;
     // rows of a tile of logits: few of them for few rows, as many as the registers hold for bf16 features, whose one
     // plane is read from LDS for two planes of weights
@@ -1139,61 +1205,42 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
         MIXGCN_RUN_T(split_kernel, w_blocks + grid_for((int64_t)pr * l.kp / 8), H, ldh, rows, labels, meta, first, pr, l.h_rows, k,
                      l.kp, top, shift, hp, y, w_blocks, W, ldw, c, l.cp, l.w_rows, wp);
         MIXGCN_LOGITS(logit_sums_kernel, class_tiles, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, class_tiles, sums, at_label);
-        // few rows: more lanes to each
-        if (pr <= 4096)
+        if (l.loss_rows == 4)
             MIXGCN_RUN(join_sums_kernel<4>, pr / 4, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
         else
             MIXGCN_RUN(join_sums_kernel<16>, pr / 16, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
         for (int q = 0; grads && q < l.col_pieces; ++q) {
             const int col0 = q * l.piece_cols;
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
-            const int cols = c - col0 < pc ? c - col0 : pc;
             MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
-            if (dH) {
-                const int64_t tiles = (int64_t)k_tiles * l.row_slabs;
-                if (bf16)
-                    MIXGCN_RUN(grad_rows_kernel<1>, tiles * ceil_div(pr, GradRows<1>::ROWS), g, l.g_rows, pc, pr, wp, l.kp, l.w_rows, col0, meta,
-                               first, l.row_slab_cols, k_tiles, l.row_slabs, q > 0, dhp);
-                else
-                    MIXGCN_RUN(grad_rows_kernel<2>, tiles * ceil_div(pr, GradRows<2>::ROWS), g, l.g_rows, pc, pr, wp, l.kp, l.w_rows, col0, meta,
-                               first, l.row_slab_cols, k_tiles, l.row_slabs, q > 0, dhp);
+            Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
+                            q > 0, dhp, l.w_slabs, dwp};
+            if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
+            const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ct * l.w_slabs : 0);
+            if (bf16 && l.w_width == 256) MIXGCN_RUN((gradients_kernel<1, 2, 4>), grid, ga);
+            else if (bf16 && l.w_width == 128) MIXGCN_RUN((gradients_kernel<1, 2, 2>), grid, ga);
+            else if (bf16) MIXGCN_RUN((gradients_kernel<1, 1, 1>), grid, ga);
+            else if (l.w_width == 128) MIXGCN_RUN((gradients_kernel<2, 2, 2>), grid, ga);
+            else MIXGCN_RUN((gradients_kernel<2, 1, 1>), grid, ga);
+
+            const bool last = q == l.col_pieces - 1, mean = loss && last && rp == l.row_pieces - 1;
+            Finish fa = {dhp, 0, l.row_slabs, pr, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
+                         k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
+            const bool r16 = l.row_slabs > 4, w16 = l.w_slabs > 4;
+            if (dH && last) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
+            if (dW) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
+            const int64_t blocks = (int64_t)fa.row_blocks + fa.w_blocks + (mean ? 1 : 0);
+            if (blocks > 0) {
+                if (r16 && w16) MIXGCN_RUN_T3(finish_kernel, 16, 16, blocks, fa);
+                else if (r16) MIXGCN_RUN_T3(finish_kernel, 16, 1, blocks, fa);
+                else if (w16) MIXGCN_RUN_T3(finish_kernel, 1, 16, blocks, fa);
+                else MIXGCN_RUN_T3(finish_kernel, 1, 1, blocks, fa);
             }
-            if (dW) {
-                const int wt = l.kp / l.w_width;
-                const int64_t grid = (int64_t)wt * ct * l.w_slabs;
-                if (bf16 && l.w_width == 256)
-                    MIXGCN_RUN((grad_weights_kernel<1, 4>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
-                else if (bf16)
-                    MIXGCN_RUN((grad_weights_kernel<1, 2>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
-                else
-                    MIXGCN_RUN((grad_weights_kernel<2, 2>), grid, hp, l.kp, l.h_rows, g, l.g_rows, pc, pr, meta, first, ct, wt, l.w_slabs, dwp);
-                const int64_t items = (int64_t)k * ceil_div(cols, 4);
-                if (l.w_slabs > 4)
-                    MIXGCN_RUN(finish_weights_kernel<16>, ceil_div(items, kBlock / 16), dwp, l.w_slabs, k, l.kp, pc, cols, shift, meta,
-                               first, rp > 0, dW + col0, ldg);
-                else
-                    MIXGCN_RUN(finish_weights_kernel<1>, ceil_div(items, kBlock), dwp, l.w_slabs, k, l.kp, pc, cols, shift, meta,
-                               first, rp > 0, dW + col0, ldg);
-            }
-        }
-        if (dH) {
-            const int64_t items = (int64_t)pr * ceil_div(k, 4);
-#define MIXGCN_FINISH(SL)                                                                                                   \
-    do {                                                                                                                    \
-        if (bf16)                                                                                                           \
-            MIXGCN_RUN((finish_rows_kernel<true, SL>), ceil_div(items, kBlock / SL), dhp, l.row_slabs, pr, k, l.kp, shift, meta, \
-                       first, rows, dH, ldd);                                                                               \
-        else                                                                                                                \
-            MIXGCN_RUN((finish_rows_kernel<false, SL>), ceil_div(items, kBlock / SL), dhp, l.row_slabs, pr, k, l.kp, shift, meta, \
-                       first, rows, dH, ldd);                                                                               \
-    } while (0)
-            if (l.row_slabs > 4) MIXGCN_FINISH(16);
-            else MIXGCN_FINISH(1);
-#undef MIXGCN_FINISH
         }
     }
-    if (loss) hipLaunchKernelGGL(mean_loss_kernel, dim3(1), dim3(1024), 0, s, losses, meta, loss);
+    if (loss && !grads) MIXGCN_RUN(mean_loss_kernel, 1, losses, l.loss_rows, meta, loss);
 #undef MIXGCN_LOGITS
+#undef MIXGCN_RUN_T3
 #undef MIXGCN_RUN_T
 #undef MIXGCN_RUN
     MIXGCN_HIP_TRY(hipGetLastError());
