@@ -1080,13 +1080,14 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     // tiles of 64 features where they are a quarter less than tiles of 128 (k up to 64, 129 to 192)
     l.kp = (int)(4 * up(k, 64) <= 3 * up(k, 128) ? up(k, 64) : up(k, 128));
     l.cp = (int)up(c, kTile);
-    // G, four bytes a logit, is handed on in blocks of 2^26 logits at most: as many classes as give dW a tile for
-    // every compute unit without a split of the rows, and rows for the rest
+    // G, four bytes a logit, is handed on in blocks of at most 2^26 logits, of 8192 classes and as many rows (us of
+    // 16384 x 512 -> 50001 bf16 and 72640 x 32 -> 8123 fp32, 2^24, 2^25, 2^26, 2^27: 8200 6820 5850 5550, 2430 1840 1670
+    // 1770; of 30000 x 200 -> 20000 bf16 with 4096 rows of 16384 classes 3080, 8192 of 8192 2630).  Where twice the rows
+    // are all of them they are one block (the first of these 5770 -> 5510).
     const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
-    int64_t cols = between(2048, up((int64_t)32768 * kTile / l.kp, kTile), 32768);
-    if (cols > l.cp) cols = l.cp;
-    int64_t rows = between(2048, most / cols / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
-    if (rows > all_rows) rows = all_rows;
+    int64_t cols = between(kTile, l.cp, 8192);
+    int64_t rows = between(kMostTileRows, most / cols / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
+    if (all_rows <= 2 * rows) rows = all_rows;
     cols = between(kTile, most / rows / kTile * kTile, l.cp);
     l.piece_rows = (int)rows;
     l.piece_cols = (int)cols;
@@ -1097,12 +1098,12 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.col_pieces = (int)ceil_div(l.cp, cols);
     l.r_width = l.kp % 128 ? 64 : 128;
     l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 ? 256 : 128;
-    // two workgroups for every compute unit
+    // a workgroup of either gradient for every compute unit
     const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
-    const int64_t s = between(1, 512 / (l.kp / l.r_width * row_tiles), col_tiles);
+    const int64_t s = between(1, 256 / (l.kp / l.r_width * row_tiles), col_tiles);
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
-    l.w_slabs = (int)between(1, 512 / (l.kp / l.w_width * col_tiles), rows / kTile);
+    l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * col_tiles), rows / kTile);
     l.loss_rows = rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
