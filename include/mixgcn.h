@@ -437,8 +437,8 @@ int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
  * and rounds x / 2^s to the nearest code, ties to even: an element is off by 2^s / 2, at most 1/127 of the group's
  * largest, and the codes do not depend on anything but x.  What is not finite is left out of s and has the code
  * -128, which is read back as NaN.  Codes of the row padding up to whole 16 bytes become zero.
- * mixgcn_checkpoint_unpack writes code * 2^s, which is a bf16 number and so exact in either type; the row padding of X
- * stays as it is.  At most 2^28 columns.
+ * mixgcn_checkpoint_unpack writes code * 2^s, which is a bf16 number and so exact in either type; the elements of X's row
+ * padding up to whole 16 bytes become zero.  At most 2^28 columns.
  */
 int mixgcn_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n_rows, int32_t n_cols, int8_t* codes,
                            int64_t ld_codes, uint8_t* exponents, int64_t ld_exponents, void* stream);
