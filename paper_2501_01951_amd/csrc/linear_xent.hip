@@ -593,11 +593,13 @@ __device__ inline int rows_here(const Meta* meta, uint32_t first, int piece_rows
 // Tiles of logits come transposed, classes x rows, so that a lane holds classes of one row: sums over the classes stay
 // in the lane, but for one exchange of its halves.  In units of log 2: t = logit * log2(e).
 //
-// A workgroup takes 128 classes (a wavefront 64) and 64 TN rows.  Tiles are walked in groups of 8 tiles of classes: their
+// A workgroup takes 128 classes (a wavefront 64) and 64 TN rows; few rows, for which there are few workgroups, have more steps on
+// their way.  Tiles are walked in groups of 8 tiles of classes: their
 // weights stay in the L2 of an XCD while the rows pass by.
 template <int TH, int TN>
 struct Logits {
-    using P = Product<2, TH, false, false, 2, TN, 2>;
+    static constexpr int STAGES = TN > 1 ? 2 : TH == 1 ? 4 : 3;
+    using P = Product<2, TH, false, false, 2, TN, STAGES>;
     static constexpr int ROWS = 64 * TN, GROUP = 8;
     int c0, r0;  // first class and row of the tile
 
@@ -860,6 +862,11 @@ struct Gradients {
     float* dh;
     int w_slabs;                               // dW: its rows are dealt to slabs
     float* dw;
+    // where that is one slab and one block of rows, dW itself takes the sums
+    float* dW;
+    int64_t ldg;
+    int k, c;
+    const int32_t* shift;
 };
 
 // Tiles of 64 TM rows x 64 TN features.  One term each (bf16 features, whose gradient is rounded to 8 bits afterwards) or two.
@@ -871,8 +878,8 @@ struct GradRows {
 
     static __device__ inline void run(const Gradients& a, uint16_t* lds)
     {
-        const int k_tiles = a.kp / P::WB;
-        const unsigned row_tiles = (unsigned)(rows_here(a.meta, a.first, a.piece_rows) + ROWS - 1) / ROWS;
+        const int k_tiles = a.kp / P::WB, live = rows_here(a.meta, a.first, a.piece_rows);
+        const unsigned row_tiles = (unsigned)(live + ROWS - 1) / ROWS;
         const unsigned tiles = row_tiles * (unsigned)(k_tiles * a.row_slabs);
         if (blockIdx.x >= tiles) return;
         const unsigned lid = xcd_local_index(blockIdx.x, tiles);
@@ -892,6 +899,7 @@ struct GradRows {
             a.dh + ((size_t)slab * a.piece_rows + r0 + wm * TM * 32) * a.kp + kt * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
         for (int x = 0; x < TM; ++x) {
+            if (r0 + (wm * TM + x) * 32 >= live) continue;
             if (a.add) {
                 // all loads of a row of tiles before its first store (left to follow each other they cost 56 us a piece)
                 float had[TN][16];
@@ -933,6 +941,22 @@ struct GradWeights {
         P::run({a.hp + ((size_t)(kt * P::WA / BK) * a.h_rows + r0) * BK, a.h_rows, (size_t)a.kp * a.h_rows},
                {a.g + ((size_t)(ct * kTile / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
                r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
+        if (a.dW) {
+            const float inv = a.meta->count ? 1.f / (float)a.meta->count : 0.f;
+            const int f0 = kt * P::WA + wm * TM * 32, col = a.col0 + ct * kTile + wn * 64 + (lane & 31);
+#pragma unroll
+            for (int x = 0; x < TM; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int f = f0 + x * 32 + tile_row(v, lane);
+                    if (f >= a.k) continue;
+                    const int e = -15 - a.shift[f];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (col + y * 32 < a.c) a.dW[(int64_t)f * a.ldg + col + y * 32] = ldexpf(acc[x][y][v] * inv, e);
+                }
+            return;
+        }
         float* const out = a.dw + ((size_t)slab * a.kp + kt * P::WA + wm * TM * 32) * a.piece_cols + ct * kTile + wn * 64 + (lane & 31);
 #pragma unroll
         for (int x = 0; x < TM; ++x)
@@ -1216,7 +1240,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     const int pieces = l.cp / kHalfTile;
     // rows of a tile of logits: few of them for few rows, as many as the registers hold for bf16 features, whose one
     // plane is read from LDS for two planes of weights
-    const int logit_rows = pr <= 256 && n <= 64 ? 64 : bf16 ? 256 : 128;
+    const int logit_rows = n <= 128 ? 64 : bf16 ? 256 : 128;
 #define MIXGCN_LOGITS(KERNEL, CLASS_TILES, ...)                                                         \
     do {                                                                                                \
         const int64_t grid = (int64_t)(CLASS_TILES) * (pr / logit_rows);                                \
@@ -1240,7 +1264,9 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
             MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
             Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
-                            q > 0, dhp, l.w_slabs, dwp};
+                            q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift};
+            const bool direct = l.w_slabs == 1 && l.row_pieces == 1;
+            if (direct) ga.dW = dW;
             if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
             const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ct * l.w_slabs : 0);
             if (bf16 && l.w_width == 256) MIXGCN_RUN((gradients_kernel<1, 2, 4>), grid, ga);
@@ -1254,7 +1280,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
                          k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
             const bool r16 = l.row_slabs > 4, w16 = l.w_slabs > 4;
             if (dH && last) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
-            if (dW) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
+            if (dW && !direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
             const int64_t blocks = (int64_t)fa.row_blocks + fa.w_blocks + (mean ? 1 : 0);
             if (blocks > 0) {
                 if (r16 && w16) MIXGCN_RUN_T3(finish_kernel, 16, 16, blocks, fa);
