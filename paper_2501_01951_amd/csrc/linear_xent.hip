@@ -446,10 +446,11 @@ __device__ inline void wait_and_meet()
 }
 // 16 bytes per lane from base + offset to LDS at lds + 16 lane (lds in bytes, the same for the wavefront).  The
 // compiler does not count this load: wait_and_meet waits for it.  (M0 is no register that the compiler keeps values in,
-// and nothing else here uses it.)
+// and nothing else here uses it.  The instruction after a write of M0 waits one state, one that takes a base from registers
+// that a vector instruction may have written waits five.)
 __device__ inline void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
 template <int TA, int TB, bool TRA, bool TRB, int TM, int TN, int STAGES>

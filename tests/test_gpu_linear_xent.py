@@ -111,8 +111,12 @@ def poisoned(mg, h, c, gradients=True):
 
 SIZES = [(1, 1, 1), (1, 4, 2), (1, 128, 1000), (3, 5, 2), (127, 33, 129), (128, 128, 128), (129, 100, 300), (300, 130, 4097),
          (1000, 64, 63), (513, 257, 700), (40, 8, 70001), (64, 602, 65), (2049, 32, 47),
-         (16400, 16, 4500),   # pieces of rows and pieces of classes, the last ones not whole
-         (140001, 8, 5)]      # pieces of rows of few classes
+         (16400, 16, 4500),   # pieces of classes, the last one not whole
+         (16700, 8, 8300),    # pieces of rows and of classes
+         (140001, 8, 5),      # many rows of few classes
+         (530001, 4, 3),      # pieces of those
+         (70, 2100, 90), (33, 5000, 260),   # more features than a block keeps the scales of
+         (96, 192, 1000), (200, 320, 129)]  # features in tiles of 64, and of 128
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -245,6 +249,20 @@ def test_all_features_zero(mg):
     mg.linear_xent(h, w, y, loss=loss, dH=dh[:, :16], dW=dw[:, :90], row_loss=row_loss)
     torch.cuda.synchronize()
     Oracle(h, w, y).all(loss, row_loss, dh[:, :16], dw[:, :90])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_another_magnitude(mg, dtype):
+    """One row 2^14 times the others, and one weight: the others' elements then have their second terms below the smallest
+    normal f16, which keep their bits.  (2^-39 of the largest in a column is below 2^-22 of the others.)"""
+    say(f"linear_xent a large row {dtype}")
+    h, w, y = inputs(300, 48, 200, DTYPES[dtype], seed=21)
+    h[17] *= 2.0 ** 14
+    w[5, 7] *= 2.0 ** 10
+    loss, row_loss, dh, dw = outputs(h, w)
+    mg.linear_xent(h, w, y, loss=loss, dH=dh[:, :48], dW=dw[:, :200], row_loss=row_loss)
+    torch.cuda.synchronize()
+    Oracle(h, w, y).all(loss, row_loss, dh[:, :48], dw[:, :200])
 
 
 @pytest.mark.parametrize("value", [float("inf"), -float("inf"), NAN])
