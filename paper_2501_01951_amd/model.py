@@ -318,9 +318,11 @@ class GCNCheckpointStep:
         need = [B.linear_xent_workspace(dt, self.n, *self.w[-1].shape)]
         need += [B.checkpoint_wgrad_workspace(self.n, *w.shape) for w in self.w[:L - 1]]
         self.workspace = torch.empty(max(need), dtype=torch.uint8, device=dev)
+        self.gradient_in_z = False
 
     def _aggregates(self, keep: bool):
         """The last layer's aggregate; with `keep`, the others' go into their checkpoints."""
+        self.gradient_in_z = False
         h = self.x
         for l, w in enumerate(self.w):
             k, m = w.shape
@@ -339,8 +341,13 @@ class GCNCheckpointStep:
         z = self._aggregates(True)
         B.linear_xent(z, self.w[-1], self.labels, loss=self.loss, dH=z if len(self.w) > 1 else None, dW=self.dw[-1],
                       workspace=self.workspace)
+        self.gradient_in_z = True
 
     def backward(self):
+        """The other layers' weight gradients.  Works on the buffers that forward left: once after each."""
+        if not self.gradient_in_z:
+            raise RuntimeError("backward: forward has not run since the last backward or score")
+        self.gradient_in_z = False
         for l in range(len(self.w) - 2, -1, -1):
             k, m = self.w[l].shape
             # dZ of the layer above through A_hat^T, times this layer's ReLU derivative
@@ -354,7 +361,8 @@ class GCNCheckpointStep:
         self.backward()
 
     def score(self, labels=None, out=None):
-        """Loss of every node (float32 [n], 0 without a label) with the present weights, for validation."""
+        """Loss of every node (float32 [n], 0 without a label) with the present weights, for validation.  Uses the
+        buffers of the step: not between forward and backward."""
         labels = self.labels if labels is None else labels
         out = torch.empty(self.n, device=self.x.device) if out is None else out
         B.linear_xent(self._aggregates(False), self.w[-1], labels, row_loss=out, workspace=self.workspace)

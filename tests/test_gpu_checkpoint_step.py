@@ -168,3 +168,23 @@ def test_captured_step(mg):
         torch.cuda.synchronize()
         assert torch.equal(step.loss, eager.loss)
         assert all(torch.equal(p, q) for p, q in zip(step.dw, eager.dw))
+
+
+def test_backward_without_its_forward(mg):
+    """The gradient that backward starts from is gone after a backward or a score."""
+    say("checkpoint step out of order")
+    g, _, x, ws, y = problem(mg, 500, (24, 32, 90), torch.float32, 9)
+    step = mg.GCNCheckpointStep(g, x, ws, y)
+    with pytest.raises(RuntimeError, match="forward"):
+        step.backward()
+    step.step()
+    with pytest.raises(RuntimeError, match="forward"):
+        step.backward()
+    step.forward()
+    step.score()
+    with pytest.raises(RuntimeError, match="forward"):
+        step.backward()
+    want = [w.clone() for w in step.dw]
+    step.step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(step.dw, want))
