@@ -627,7 +627,7 @@ int mixgcn_checkpoint_unpack(int dtype, const int8_t* codes, int64_t ld_codes, c
 
 int64_t mixgcn_checkpoint_wgrad_workspace(int64_t n_rows, int32_t k, int32_t m)
 {
-    if (n_rows < 0 || k <= 0 || m <= 0) return -1;
+    if (n_rows < 0 || k <= 0 || k > kMostCheckpointCols || m <= 0) return -1;
     return checkpoint_wgrad_bytes(n_rows, k, m);
 }
 

@@ -420,8 +420,8 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 // [j / 32][i][j % 32], with `rows` rows to a block.  A product takes one with the reduction along its columns (a step of
 // 32 is a block, tile rows times 64 contiguous bytes), or, TR, along its rows (a step is 32 rows of each of the tile's
 // blocks, 2 KB contiguous); the transposing LDS read turns the latter: lane i of 16 receives element i % 4 of the 8 bytes
-// that lanes i / 4, + 4, + 8 and + 12 address.  (With plain rows, of which a step takes 64 bytes each, the product
-// of 7800 x 7150 gradients and 7150 x 512 weights took 137 us.)
+// that lanes i / 4, + 4, + 8 and + 12 address.  (With plain rows, of which a step takes 64 bytes each, the second pass over
+// the logits of 16384 x 512 -> 50001 bf16 took 1956 us instead of 1676, the product for dH 1923 instead of 1674.)
 //
 // Sums of A[i][k] B[k][j] over a tile of 64 TM x 64 TN, on 2 x 2 wavefronts of 32 TM x 32 TN.  Steps go straight from
 // memory to LDS, 16 bytes per lane and 1 KB per instruction, STAGES - 1 of them ahead; there is one barrier per step,
@@ -1114,6 +1114,7 @@ struct Layout {
     int row_pieces, col_pieces;
     int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
     int w_slabs;                    // dW: rows of a piece dealt to slabs
+    bool direct;                    // ... whose product writes dW itself
     int r_width, w_width;           // features of a tile of dH, of dW
     int loss_rows;                  // rows of a partial sum of the losses
     int list_step, list_blocks;
@@ -1136,7 +1137,9 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     // are all of them they are one block (the first of these 5770 -> 5510).
     const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
     int64_t cols = between(kTile, l.cp, 8192);
-    int64_t rows = between(kMostTileRows, most / cols / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
+    // (2^18 rows at most, and 2^32 cells of dH: a launch has less than 2^32 threads)
+    const int64_t most_rows = between(kMostTileRows, ((int64_t)1 << 32) / l.kp / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
+    int64_t rows = between(kMostTileRows, most / cols / kMostTileRows * kMostTileRows, most_rows);
     if (all_rows <= 2 * rows) rows = all_rows;
     cols = between(kTile, most / rows / kTile * kTile, l.cp);
     l.piece_rows = (int)rows;
@@ -1154,6 +1157,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
     l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * col_tiles), rows / kTile);
+    l.direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
@@ -1179,7 +1183,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     if (gradients) {
         l.g = take((size_t)2 * l.g_rows * cols * 2);
         l.dh = take((size_t)l.row_slabs * rows * l.kp * 4);
-        l.dw = take((size_t)l.w_slabs * l.kp * cols * 4);
+        l.dw = take(l.direct ? 0 : (size_t)l.w_slabs * l.kp * cols * 4);
     }
     l.bytes = at;
     return l;
@@ -1266,8 +1270,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
             Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
                             q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift};
-            const bool direct = l.w_slabs == 1 && l.row_pieces == 1;
-            if (direct) ga.dW = dW;
+            if (l.direct) ga.dW = dW;
             if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
             const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ct * l.w_slabs : 0);
             if (bf16 && l.w_width == 256) MIXGCN_RUN((gradients_kernel<1, 2, 4>), grid, ga);
@@ -1281,7 +1284,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
                          k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
             const bool r16 = l.row_slabs > 4, w16 = l.w_slabs > 4;
             if (dH && last) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
-            if (dW && !direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
+            if (dW && !l.direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
             const int64_t blocks = (int64_t)fa.row_blocks + fa.w_blocks + (mean ? 1 : 0);
             if (blocks > 0) {
                 if (r16 && w16) MIXGCN_RUN_T3(finish_kernel, 16, 16, blocks, fa);

@@ -142,3 +142,16 @@ def test_wrappers_refuse_what_does_not_fit():
         mg.checkpoint_wgrad(kept, torch.zeros(4, 8), torch.zeros(40, 9))
     with pytest.raises(ValueError):
         mg.checkpoint_wgrad(kept, torch.zeros(4, 8), torch.zeros(40, 8), mask=torch.zeros(3, 1, dtype=torch.int32))
+
+
+def test_workspaces_of_many_columns(lib):
+    """A product that writes its result itself has no slabs in the workspace, many features shorten a block of rows so that no
+    launch has 2^32 threads, and sizes that multiply past 64 bits are bad ones."""
+    f = lib.mixgcn_linear_xent_workspace
+    k, c = 1 << 12, 1 << 18
+    assert f(0, 200, k, c, 1) < 1.05 * (4 * k * c) + (1 << 27) + 4 * 256 * (c + k * 2) + 8 * 256 * c // 64
+    for dtype, planes in ((0, 2), (1, 1)):
+        n, k = 1 << 19, 1 << 15
+        assert f(dtype, n, k, 100, 1) < (1 << 17) * k * (2 * planes + 4) + (1 << 28)
+    assert lib.mixgcn_checkpoint_wgrad_workspace(1, (1 << 28) + 1, 1) == -1
+    assert lib.mixgcn_checkpoint_wgrad_workspace(1, 1 << 28, 0x7FFFFFFF) == (1 << 30) * 0x7FFFFFFF
