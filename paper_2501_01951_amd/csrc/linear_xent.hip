@@ -59,10 +59,13 @@ __device__ inline uint32_t labelled4(const int32_t* labels, int64_t r, int64_t e
     return have;
 }
 
+// The labels of each block of list_labels.  Clears the maxima of the features.
 __global__ __launch_bounds__(kBlock) void count_labels_kernel(const int32_t* __restrict__ labels, int64_t n, int32_t c,
-                                                              int per_block, uint32_t* __restrict__ counts)
+                                                              int per_block, uint32_t* __restrict__ counts,
+                                                              uint32_t* __restrict__ top, int n_top)
 {
     __shared__ uint32_t part[kBlock / kWave];
+    for (int i = blockIdx.x * kBlock + threadIdx.x; i < n_top; i += gridDim.x * kBlock) top[i] = 0u;
     const int64_t r0 = (int64_t)blockIdx.x * per_block, end = r0 + per_block < n ? r0 + per_block : n;
     uint32_t mine = 0;
     for (int64_t r = r0 + 4 * threadIdx.x; r < end; r += kListStep) mine += __popc(labelled4(labels, r, end, c));
@@ -73,19 +76,17 @@ __global__ __launch_bounds__(kBlock) void count_labels_kernel(const int32_t* __r
     if (threadIdx.x == 0) counts[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
-// rows[i]: the i-th row with a label.  Clears the maxima of the features.
-__global__ __launch_bounds__(kBlock) void list_labels_kernel(const int32_t* __restrict__ labels, int64_t n, int32_t c,
-                                                             int per_block, const uint32_t* __restrict__ counts,
-                                                             uint32_t* __restrict__ rows, Meta* __restrict__ meta,
-                                                             uint32_t* __restrict__ top, int n_top)
+// rows[i]: the i-th row with a label, for block `block` of `blocks`.
+__device__ inline void list_labels(int block, int blocks, const int32_t* __restrict__ labels, int64_t n, int32_t c, int per_block,
+                                   const uint32_t* __restrict__ counts, uint32_t* __restrict__ rows, Meta* __restrict__ meta)
 {
     __shared__ uint64_t lds[4];
     const int tid = threadIdx.x;
     uint64_t before = 0;
-    for (unsigned b = tid; b < blockIdx.x; b += kBlock) before += counts[b];
+    for (int b = tid; b < block; b += kBlock) before += counts[b];
     uint64_t base = 0;
-    if (blockIdx.x > 0) block_exclusive_scan_u64(before, &base, lds);
-    const int64_t r0 = (int64_t)blockIdx.x * per_block, end = r0 + per_block < n ? r0 + per_block : n;
+    if (block > 0) block_exclusive_scan_u64(before, &base, lds);
+    const int64_t r0 = (int64_t)block * per_block, end = r0 + per_block < n ? r0 + per_block : n;
     for (int64_t s = r0; s < end; s += kListStep) {
         const int64_t r = s + 4 * tid;
         const uint32_t have = labelled4(labels, r, end, c);
@@ -96,9 +97,7 @@ __global__ __launch_bounds__(kBlock) void list_labels_kernel(const int32_t* __re
             if (have >> i & 1u) rows[at++] = (uint32_t)(r + i);
         base += total;
     }
-    if (blockIdx.x == gridDim.x - 1 && tid == 0) meta->count = (uint32_t)base;
-    if (blockIdx.x == 0)
-        for (int i = tid; i < n_top; i += kBlock) top[i] = 0u;
+    if (block == blocks - 1 && tid == 0) meta->count = (uint32_t)base;
 }
 
 // ---- scales -------------------------------------------------------------------------------------
@@ -178,25 +177,33 @@ constexpr int kTopWidth = 8 * kBlock;  // columns of H that a block takes at a t
 
 // What the roles of the blocks of top_kernel are.
 struct TopPlan {
-    int w_blocks, w_pieces;   // maxima of the rows of W
-    int h_blocks, h_rows;     // maxima of the columns of H, h_rows listed rows to a block
-    int clear_blocks;         // zeros for the rows without a label
+    int list_blocks, list_step;  // the list of the rows with a label
+    int w_blocks, w_pieces;      // maxima of the rows of W
+    int h_blocks, h_rows;        // maxima of the columns of H, h_rows rows to a block
+    int clear_blocks;            // zeros for the rows without a label
+    bool alone;                  // every maximum is found by one block, and nothing has cleared them
 };
 
-// top[k]: largest magnitude of column k of H over the rows with a label; top[kp + k]: of row k of W.  (Maxima do not
-// depend on the order of the atomics.)  And, beside that, zeros for the rows without a label, of dH (if it is given) and of
-// the losses of the rows.
+// What a call begins with: the list of the rows with a label; top[k], the largest magnitude of column k of H over these
+// rows, and top[kp + k], of row k of W (maxima do not depend on the order of the atomics); zeros for the other rows of
+// dH (if it is given) and of the losses of the rows.
+// (The list in a launch of its own before this one: 1 x 128 -> 1000 LIST1, 10007 x 256 -> 5003 bf16 LIST2.)
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H, int64_t ldh,
-                                                     const uint32_t* __restrict__ rows, const Meta* __restrict__ meta,
-                                                     const float* __restrict__ W, int64_t ldw, int k, int c, int kp,
-                                                     TopPlan plan, uint32_t* __restrict__ top,
-                                                     const int32_t* __restrict__ labels, int64_t n, void* __restrict__ dH,
+                                                     const uint32_t* __restrict__ counts, uint32_t* __restrict__ rows,
+                                                     Meta* __restrict__ meta, const float* __restrict__ W, int64_t ldw, int k,
+                                                     int c, int kp, TopPlan plan, uint32_t* __restrict__ top,
+                                                     const int32_t* __restrict__ labels, int64_t n, void* dH,
                                                      int64_t ldd, float* __restrict__ row_loss)
 {
     __shared__ uint32_t col_top[kTopWidth];
     const int tid = threadIdx.x;
     int b = blockIdx.x;
+    if (b < plan.list_blocks) {
+        list_labels(b, plan.list_blocks, labels, n, c, plan.list_step, counts, rows, meta);
+        return;
+    }
+    b -= plan.list_blocks;
     if (b < plan.w_blocks) {
         const int row = b / plan.w_pieces, c0 = b % plan.w_pieces * kTopCols;
         const float* const w = W + (int64_t)row * ldw;
@@ -227,33 +234,48 @@ __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H,
         if (tid == 0) {
 #pragma unroll
             for (int i = 1; i < kBlock / kWave; ++i) m = col_top[i] > m ? col_top[i] : m;
-            atomicMax(top + kp + row, m);
+            if (plan.alone) top[kp + row] = m;
+            else atomicMax(top + kp + row, m);
         }
     } else if (b < plan.w_blocks + plan.h_blocks) {
-        const uint32_t count = meta->count, i0 = (uint32_t)(b - plan.w_blocks) * (uint32_t)plan.h_rows;
-        const int m_rows = i0 >= count ? 0 : count - i0 < (uint32_t)plan.h_rows ? (int)(count - i0) : plan.h_rows;
-        for (int j0 = 0; j0 < k && m_rows > 0; j0 += kTopWidth) {
+        const int64_t i0 = (int64_t)(b - plan.w_blocks) * plan.h_rows;
+        const int m_rows = n - i0 < plan.h_rows ? (int)(n - i0) : plan.h_rows;
+        for (int j0 = 0; j0 < k; j0 += kTopWidth) {
             const int width = k - j0 < kTopWidth ? k - j0 : kTopWidth;
             const int lanes = (width + 7) / 8, at_once = kBlock / lanes;
             for (int i = tid; i < width; i += kBlock) col_top[i] = 0u;
             __syncthreads();
             const int j = 8 * (tid % lanes);
             uint32_t m[8] = {};
+            constexpr int U = 4;
             if (tid < at_once * lanes)
-                for (int i = tid / lanes; i < m_rows; i += at_once) {
-                    Eight<BF16> x;
-                    x.load(H, (int64_t)rows[i0 + i] * ldh, j0 + j, ldh);
+                for (int i = tid / lanes; i < m_rows; i += U * at_once) {
+                    bool have[U];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t t = magnitude(x.get(e));
-                        m[e] = t > m[e] ? t : m[e];
+                    for (int u = 0; u < U; ++u) {
+                        const int iu = i + u * at_once;
+                        have[u] = iu < m_rows && has_label(labels[i0 + (iu < m_rows ? iu : i)], c);
                     }
+                    Eight<BF16> x[U] = {};
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (have[u]) x[u].load(H, (i0 + i + u * at_once) * ldh, j0 + j, ldh);
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t t = magnitude(x[u].get(e));
+                            m[e] = t > m[e] ? t : m[e];
+                        }
                 }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (j + e < width && m[e]) atomicMax(&col_top[j + e], m[e]);
             __syncthreads();
-            for (int i = tid; i < width; i += kBlock) atomicMax(top + j0 + i, col_top[i]);
+            for (int i = tid; i < width; i += kBlock) {
+                if (plan.alone) top[j0 + i] = col_top[i];
+                else if (col_top[i]) atomicMax(top + j0 + i, col_top[i]);
+            }
             __syncthreads();
         }
     } else {
@@ -357,8 +379,8 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
     if (blockIdx.x == 0) {
         // for the kernels that follow
         for (int i = threadIdx.x; i < kp; i += kBlock) {
-            shift[i] = scale_of(top[i], top[kp + i], most);
-            shift[kp + i] = scale_of(top[kp + i], top[i], most, true);
+            shift[i] = i < k ? scale_of(top[i], top[kp + i], most) : 0;
+            shift[kp + i] = i < k ? scale_of(top[kp + i], top[i], most, true) : 0;
         }
         if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most - 28);
     }
@@ -863,11 +885,14 @@ struct Gradients {
     float* dh;
     int w_slabs;                               // dW: its rows are dealt to slabs
     float* dw;
-    // where that is one slab and one block of rows, dW itself takes the sums
+    // where that is one slab and one block of rows, dW itself takes the sums, and dH where it is one slab and one block of classes
     float* dW;
     int64_t ldg;
     int k, c;
     const int32_t* shift;
+    void* dH;
+    int64_t ldd;
+    const uint32_t* rows;
 };
 
 // Tiles of 64 TM rows x 64 TN features.  One term each (bf16 features, whose gradient is rounded to 8 bits afterwards) or two.
@@ -876,6 +901,49 @@ struct GradRows {
     static constexpr int TM = T == 1 ? 4 : 2, STAGES = T == 1 ? 3 : 2;
     using P = Product<T, T, false, true, TM, TN, STAGES>;
     static constexpr int ROWS = 64 * TM;
+
+    // Rows of dH from the wavefront's sums, of features f0 on and listed rows r0 on.
+    static __device__ inline void write(const Gradients& a, int r0, int live, int f0, int lane, const floatx16 (&acc)[TM][TN])
+    {
+        const float inv = 1.f / (float)a.meta->count;
+        const int f = f0 + (lane & 31);
+        int e[TN];
+#pragma unroll
+        for (int y = 0; y < TN; ++y) e[y] = -15 - a.shift[a.kp + f + y * 32];
+#pragma unroll
+        for (int x = 0; x < TM; ++x) {
+            if (r0 + x * 32 >= live) continue;
+            uint32_t row[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int r = r0 + x * 32 + tile_row(v, lane);
+                row[v] = a.rows[a.first + (r < live ? r : live - 1)];
+            }
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; v += 2) {
+                    const float g0 = ldexpf(acc[x][y][v] * inv, e[y]), g1 = ldexpf(acc[x][y][v + 1] * inv, e[y]);
+                    const int r = r0 + x * 32 + tile_row(v, lane), col = f + y * 32;
+                    if (T == 1) {
+                        // neighboring lanes exchange, so that each has two features of one of the rows
+                        const bool odd = lane & 1;
+                        const int send = __float_as_int(odd ? g0 : g1);
+                        const float got = __int_as_float(__builtin_amdgcn_update_dpp(send, send, 0xB1, 0xF, 0xF, false));
+                        const uint32_t w = odd ? pack_bf16(got, g1) : pack_bf16(g0, got);
+                        const int c0 = col & ~1;
+                        if (r + (odd ? 1 : 0) >= live) continue;
+                        uint16_t* const o = (uint16_t*)a.dH + (int64_t)(odd ? row[v + 1] : row[v]) * a.ldd + c0;
+                        if (c0 + 1 < a.k) *reinterpret_cast<uint32_t*>(o) = w;
+                        else if (c0 < a.k) *o = (uint16_t)w;
+                    } else if (col < a.k) {
+                        float* const o = (float*)a.dH + col;
+                        if (r < live) o[(int64_t)row[v] * a.ldd] = g0;
+                        if (r + 1 < live) o[(int64_t)row[v + 1] * a.ldd] = g1;
+                    }
+                }
+        }
+    }
 
     static __device__ inline void run(const Gradients& a, uint16_t* lds)
     {
@@ -896,6 +964,10 @@ struct GradRows {
         P::run({a.g + ((size_t)(s0 / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
                {a.wp + ((size_t)(kt * P::WB / BK) * a.w_rows + a.col0 + s0) * BK, a.w_rows, (size_t)a.kp * a.w_rows},
                s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
+        if (a.dH) {
+            write(a, r0 + wm * TM * 32, live, kt * P::WB + wn * TN * 32, lane, acc);
+            return;
+        }
         float* const out =
             a.dh + ((size_t)slab * a.piece_rows + r0 + wm * TM * 32) * a.kp + kt * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
@@ -1114,7 +1186,7 @@ struct Layout {
     int row_pieces, col_pieces;
     int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
     int w_slabs;                    // dW: rows of a piece dealt to slabs
-    bool direct;                    // ... whose product writes dW itself
+    bool rows_direct, w_direct;     // the product writes dH, dW itself
     int r_width, w_width;           // features of a tile of dH, of dW
     int loss_rows;                  // rows of a partial sum of the losses
     int list_step, list_blocks;
@@ -1157,7 +1229,8 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
     l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * col_tiles), rows / kTile);
-    l.direct = l.w_slabs == 1 && l.row_pieces == 1;
+    l.rows_direct = l.row_slabs == 1 && l.col_pieces == 1;
+    l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
@@ -1182,8 +1255,8 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.g = l.dh = l.dw = 0;
     if (gradients) {
         l.g = take((size_t)2 * l.g_rows * cols * 2);
-        l.dh = take((size_t)l.row_slabs * rows * l.kp * 4);
-        l.dw = take(l.direct ? 0 : (size_t)l.w_slabs * l.kp * cols * 4);
+        l.dh = take(l.rows_direct ? 0 : (size_t)l.row_slabs * rows * l.kp * 4);
+        l.dw = take(l.w_direct ? 0 : (size_t)l.w_slabs * l.kp * cols * 4);
     }
     l.bytes = at;
     return l;
@@ -1231,16 +1304,18 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
         if (bf16) MIXGCN_RUN((KERNEL<true, R, W>), GRID, __VA_ARGS__); \
         else MIXGCN_RUN((KERNEL<false, R, W>), GRID, __VA_ARGS__);     \
     } while (0)
-    if (l.list_blocks > 1) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts);
-    MIXGCN_RUN(list_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, rows, meta, top, 2 * l.kp);
     TopPlan tp;
+    tp.list_blocks = l.list_blocks;
+    tp.list_step = l.list_step;
     tp.w_pieces = (int)ceil_div(c, kTopCols);
     tp.w_blocks = tp.w_pieces * k;
     tp.h_rows = (int)between(64, ceil_div(n, 1024), (int64_t)1 << 30);
-    tp.h_blocks = (int)ceil_div(n, tp.h_rows);
+    tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 1024);
     tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), kBlock), 4096) : 0;
-    MIXGCN_RUN_T(top_kernel, tp.w_blocks + tp.h_blocks + tp.clear_blocks, H, ldh, rows, meta, W, ldw, k, c, l.kp, tp, top, labels,
-                 n, dH, ldd, row_loss);
+    tp.alone = tp.list_blocks == 1 && tp.w_pieces == 1 && tp.h_blocks == 1;
+    if (!tp.alone) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, top, 2 * l.kp);
+    MIXGCN_RUN_T(top_kernel, tp.list_blocks + tp.w_blocks + tp.h_blocks + tp.clear_blocks, H, ldh, counts, rows, meta, W, ldw, k, c,
+                 l.kp, tp, top, labels, n, dH, ldd, row_loss);
     const int nk = (int)ceil_div(k, BK), class_tiles = l.cp / kTile, pr = l.piece_rows;
     const int pieces = l.cp / kHalfTile;
     // rows of a tile of logits: few of them for few rows, as many as the registers hold for bf16 features, whose one
@@ -1269,8 +1344,9 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
             MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
             Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
-                            q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift};
-            if (l.direct) ga.dW = dW;
+                            q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift, nullptr, ldd, rows};
+            if (l.w_direct) ga.dW = dW;
+            if (l.rows_direct) ga.dH = dH;
             if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
             const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ct * l.w_slabs : 0);
             if (bf16 && l.w_width == 256) MIXGCN_RUN((gradients_kernel<1, 2, 4>), grid, ga);
@@ -1283,8 +1359,8 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             Finish fa = {dhp, 0, l.row_slabs, pr, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
                          k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
             const bool r16 = l.row_slabs > 4, w16 = l.w_slabs > 4;
-            if (dH && last) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
-            if (dW && !l.direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
+            if (dH && last && !l.rows_direct) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
+            if (dW && !l.w_direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
             const int64_t blocks = (int64_t)fa.row_blocks + fa.w_blocks + (mean ? 1 : 0);
             if (blocks > 0) {
                 if (r16 && w16) MIXGCN_RUN_T3(finish_kernel, 16, 16, blocks, fa);
