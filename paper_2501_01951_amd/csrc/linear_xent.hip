@@ -382,7 +382,8 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
             shift[i] = i < k ? scale_of(top[i], top[kp + i], most) : 0;
             shift[kp + i] = i < k ? scale_of(top[kp + i], top[i], most, true) : 0;
         }
-        if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most - 28);
+        // (not down to zero, which would make NaN of the -infinity past the classes: 2^-100 already leaves all logits at zero)
+        if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most < -72 ? -100 : most - 28);
     }
     const bool weights = (int)blockIdx.x < w_blocks;
     for (int i = threadIdx.x; i < k && i < kScaleCols; i += kBlock)

@@ -333,3 +333,18 @@ def test_captured_and_replayed(mg):
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(o, eager))
             assert torch.isfinite(o[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [40, 200, 700])
+def test_products_below_the_smallest_float(mg, c, dtype):
+    """All logits vanish, the loss is that of even odds, and the gradients are in the range of the operands."""
+    say(f"linear_xent products below the smallest float c={c} {dtype}")
+    h, w, y = inputs(300, 36, c, DTYPES[dtype], seed=22)
+    h.mul_(2.0 ** -84)
+    w.mul_(2.0 ** -66)
+    loss, row_loss, dh, dw = outputs(h, w)
+    mg.linear_xent(h, w, y, loss=loss, dH=dh[:, :36], dW=dw[:, :c], row_loss=row_loss)
+    torch.cuda.synchronize()
+    Oracle(h, w, y).all(loss, row_loss, dh[:, :36], dw[:, :c])
+    assert (dh[:, :36] != 0).any() and (dw[:, :c] != 0).any()
