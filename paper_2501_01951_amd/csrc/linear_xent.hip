@@ -187,7 +187,8 @@ struct TopPlan {
 // What a call begins with: the list of the rows with a label; top[k], the largest magnitude of column k of H over these
 // rows, and top[kp + k], of row k of W (maxima do not depend on the order of the atomics); zeros for the other rows of
 // dH (if it is given) and of the losses of the rows.
-// (The list in a launch of its own before this one: 1 x 128 -> 1000 LIST1, 10007 x 256 -> 5003 bf16 LIST2.)
+// (With the list in a launch of its own before this one 1 x 128 -> 1000 took 23 us instead of 19, 10007 x 256 -> 5003 bf16 86
+// instead of 80.)
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H, int64_t ldh,
                                                      const uint32_t* __restrict__ counts, uint32_t* __restrict__ rows,
@@ -789,6 +790,41 @@ __global__ __launch_bounds__(kBlock) void mean_loss_kernel(const double* __restr
 }
 
 // ---- gradient with respect to the logits --------------------------------------------------------
+
+// The two terms of a 32 x 32 tile of G, from registers as the matrix instruction leaves them to its place in either plane.  tmp:
+// 4 KB that only this wavefront uses.
+__device__ inline void store_grad(const float (&g)[16], float minus_one, int lane, uint16_t* tmp, uint16_t* o, size_t plane)
+{
+    // groups of 8 classes, of which this lane has the four at 4 (lane / 32)
+    uint32_t hi[8], lo[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        hi[p] = pack_f16(g[2 * p], g[2 * p + 1]);
+        lo[p] = pack_rests(g[2 * p], g[2 * p + 1], hi[p], minus_one);
+    }
+    // The halves of the wavefront exchange, so that each has eight classes of a row, and the 32 rows of 64 bytes go
+    // through LDS into the order they have in memory (piece p of row r at p ^ (r / 4 % 4)): a store is then 1 KB in a
+    // row (72640 x 32 -> 8123 fp32 1518 -> 1479 us).
+    auto put = [&](uint16_t* to, uint16_t* t, const uint32_t (&w)[8]) {
+#pragma unroll
+        for (int q = 0; q < 8; q += 4) {
+            const auto s0 = __builtin_amdgcn_permlane32_swap(w[q], w[q + 2], false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(w[q + 1], w[q + 3], false, false);
+            const uintx4 v = {s0[0], s1[0], s0[1], s1[1]};
+            const int r = lane & 31, p = q / 2 + (lane >> 5);
+            *(lds_uintx4*)(t + r * BK + 8 * (p ^ (r >> 2 & 3))) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 16 * i + lane / 4, p = lane % 4;
+            const uintx4 v = *(lds_uintx4*)(t + r * BK + 8 * (p ^ (r >> 2 & 3)));
+            *reinterpret_cast<uint4*>(to + i * 512) = make_uint4(v.x, v.y, v.z, v.w);
+        }
+    };
+    put(o, tmp, hi);
+    put(o + plane, tmp + 1024, lo);
+}
+
 // planes[t], rows the listed ones and columns the classes from col0 on: 2^15 (softmax - onehot), zeros past the classes
 // and past the rows up to a whole tile.
 template <int TH, int TN>
@@ -839,35 +875,117 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
                     if (at == i) g[v] -= kGradScale;
                     if (cw + i >= c) g[v] = 0.f;
                 }
-            // groups of 8 classes, of which this lane has the four at 4 (lane / 32)
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                hi[p] = pack_f16(g[2 * p], g[2 * p + 1]);
-                lo[p] = pack_rests(g[2 * p], g[2 * p + 1], hi[p], minus_one);
-            }
-            // The halves of the wavefront exchange, so that each has eight classes of a row, and the 32 rows of 64 bytes go
-            // through LDS into the order they have in memory (piece p of row r at p ^ (r / 4 % 4)): a store is then 1 KB in a
-            // row (72640 x 32 -> 8123 fp32 1518 -> 1479 us).
-            auto put = [&](uint16_t* o, uint16_t* tmp, const uint32_t (&w)[8]) {
-#pragma unroll
-                for (int q = 0; q < 8; q += 4) {
-                    const auto s0 = __builtin_amdgcn_permlane32_swap(w[q], w[q + 2], false, false);
-                    const auto s1 = __builtin_amdgcn_permlane32_swap(w[q + 1], w[q + 3], false, false);
-                    const uintx4 v = {s0[0], s1[0], s0[1], s1[1]};
-                    const int r = lane & 31, p = q / 2 + (lane >> 5);
-                    *(lds_uintx4*)(tmp + r * BK + 8 * (p ^ (r >> 2 & 3))) = v;
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 16 * i + lane / 4, p = lane % 4;
-                    const uintx4 v = *(lds_uintx4*)(tmp + r * BK + 8 * (p ^ (r >> 2 & 3)));
-                    *reinterpret_cast<uint4*>(o + (size_t)x * g_rows * BK + i * 512) = make_uint4(v.x, v.y, v.z, v.w);
-                }
-            };
-            put(out, mine + (2 * x) * 1024, hi);
-            put(out + plane, mine + (2 * x + 1) * 1024, lo);
+            store_grad(g, minus_one, lane, mine + 2 * x * 1024, out + (size_t)x * g_rows * BK, plane);
         }
+    }
+}
+
+// Few classes, all in one tile: a workgroup has its rows' logits at once, and their losses and G come from one pass over them.
+// (262144 x 128 -> 172 fp32 506 -> 428 us, of 2000 x 100 -> 220 bf16 54 -> 38, of 262144 x 128 -> 47 380 -> 309.)  losses: a
+// sum per 64 rows.  planes may be null.
+template <int TH, int TM, int TN>
+__global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
+                                                               const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
+                                                               const Meta* __restrict__ meta, uint32_t first, int piece_rows,
+                                                               const uint32_t* __restrict__ rows, double* __restrict__ losses,
+                                                               float* __restrict__ row_loss, int g_rows, uint16_t* __restrict__ planes)
+{
+    constexpr int STEP = 64 * BK * (2 * TM + TH * TN), MOST = 40960 / STEP;  // halfwords
+    using P = Product<2, TH, false, false, TM, TN, MOST < 4 ? MOST : 4>;
+    constexpr int ROWS = 64 * TN;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[P::LDS];
+    static_assert(P::LDS >= 4 * 2048 + 2 * 5 * ROWS, "LDS of the end");
+    const int live = rows_here(meta, first, piece_rows), r0 = blockIdx.x * ROWS;
+    if (r0 >= live) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+    floatx16 acc[TM][TN];
+    clear(acc);
+    P::run({Wp, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds, acc);
+    const float a2 = meta->alpha * kLog2e;
+    uint16_t* const mine = lds + wave * 2048;
+    float(*const tops)[ROWS] = reinterpret_cast<float(*)[ROWS]>(lds + 4 * 2048);  // of the two halves of the classes
+    float(*const sums)[ROWS] = tops + 2;
+    float* const at_label = sums[2];
+    __syncthreads();
+    const int cw = wm * TM * 32;
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+        if (cw + (x + 1) * 32 > c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (cw + x * 32 + tile_row(v, lane) >= c)
+#pragma unroll
+                    for (int yy = 0; yy < TN; ++yy) acc[x][yy][v] = -INFINITY;
+#pragma unroll
+    for (int yy = 0; yy < TN; ++yy) {
+        const int row = (wn * TN + yy) * 32 + (lane & 31), at = y[r0 + row] - cw;
+        float most = -INFINITY, label = 0.f;
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                most = fmaxf(most, acc[x][yy][v]);
+                if (at == x * 32 + tile_row(v, lane)) label = acc[x][yy][v];
+            }
+        most = fmaxf(most, __shfl_xor(most, 32, kWave));
+        if (lane < 32) tops[wm][row] = most;
+        if (at >= 0 && at < TM * 32 && (at >> 2 & 1) == lane >> 5) at_label[row] = label;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int yy = 0; yy < TN; ++yy) {
+        const int row = (wn * TN + yy) * 32 + (lane & 31);
+        const float most = fmaxf(tops[0][row], tops[1][row]), base = most == -INFINITY ? 0.f : most * a2;
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                acc[x][yy][v] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -base));
+                sum += acc[x][yy][v];
+            }
+        sum += __shfl_xor(sum, 32, kWave);
+        if (most == -INFINITY) sum = __uint_as_float(0x7FC00000u);
+        if (lane < 32) sums[wm][row] = sum;
+    }
+    __syncthreads();
+    if (planes) {
+        float minus_one = -1.f;
+        asm("" : "+v"(minus_one));
+        const size_t plane = (size_t)(64 * TM) * g_rows;
+#pragma unroll
+        for (int yy = 0; yy < TN; ++yy) {
+            const int row = (wn * TN + yy) * 32 + (lane & 31), at = y[r0 + row] - cw;
+            // rows past the last one have no gradient
+            const float unit = r0 + row < live ? kGradScale / (sums[0][row] + sums[1][row]) : 0.f;
+            uint16_t* const out = planes + ((size_t)(wm * TM) * g_rows + r0 + (wn * TN + yy) * 32) * BK + 8 * lane;
+#pragma unroll
+            for (int x = 0; x < TM; ++x) {
+                float g[16];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    g[v] = acc[x][yy][v] * unit;
+                    if (at == x * 32 + tile_row(v, lane)) g[v] -= kGradScale;
+                }
+                if (cw + (x + 1) * 32 > c)  // where the row is not a number
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (cw + x * 32 + tile_row(v, lane) >= c) g[v] = 0.f;
+                store_grad(g, minus_one, lane, mine, out + (size_t)x * g_rows * BK, plane);
+            }
+        }
+    }
+    if (threadIdx.x < ROWS) {
+        const int row = threadIdx.x, r = r0 + row;
+        double l = 0.0;
+        if (r < live) {
+            const float f = ((fmaxf(tops[0][row], tops[1][row]) - at_label[row]) * a2 + log2f(sums[0][row] + sums[1][row])) * kLn2;
+            if (row_loss) row_loss[rows[first + r]] = f;
+            l = (double)f;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, kWave);
+        if (lane == 0 && r < live) losses[first / 64 + blockIdx.x * TN + wave] = l;
     }
 }
 
@@ -1189,6 +1307,7 @@ struct Layout {
     int w_slabs;                    // dW: rows of a piece dealt to slabs
     bool rows_direct, w_direct;     // the product writes dH, dW itself
     int r_width, w_width;           // features of a tile of dH, of dW
+    bool one_tile;                  // all classes are in one tile of logits
     int loss_rows;                  // rows of a partial sum of the losses
     int list_step, list_blocks;
     size_t meta, counts, rows, top, shift, hp, wp, y, sums, at_label, norm, losses, g, dh, dw, bytes;
@@ -1213,7 +1332,9 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     // (2^18 rows at most, and 2^32 cells of dH: a launch has less than 2^32 threads)
     const int64_t most_rows = between(kMostTileRows, ((int64_t)1 << 32) / l.kp / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
     int64_t rows = between(kMostTileRows, most / cols / kMostTileRows * kMostTileRows, most_rows);
-    if (all_rows <= 2 * rows) rows = all_rows;
+    l.one_tile = l.cp <= 2 * kTile;
+    if (all_rows <= 2 * rows && !l.one_tile) rows = all_rows;
+    if (all_rows < rows) rows = all_rows;
     cols = between(kTile, most / rows / kTile * kTile, l.cp);
     l.piece_rows = (int)rows;
     l.piece_cols = (int)cols;
@@ -1232,7 +1353,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * col_tiles), rows / kTile);
     l.rows_direct = l.row_slabs == 1 && l.col_pieces == 1;
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
-    l.loss_rows = rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
+    l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
     size_t at = 0;
@@ -1249,9 +1370,9 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.hp = take((size_t)l.terms * l.h_rows * l.kp * 2);
     l.wp = take((size_t)2 * l.kp * l.w_rows * 2);
     l.y = take((size_t)rows * 4);
-    l.sums = take((size_t)(l.cp / kHalfTile) * rows * 8);
-    l.at_label = take((size_t)rows * 4);
-    l.norm = take((size_t)rows * 8);
+    l.sums = take(l.one_tile ? 0 : (size_t)(l.cp / kHalfTile) * rows * 8);
+    l.at_label = take(l.one_tile ? 0 : (size_t)rows * 4);
+    l.norm = take(l.one_tile ? 0 : (size_t)rows * 8);
     l.losses = take((size_t)(ceil_div(n, l.loss_rows) + 1) * 8);
     l.g = l.dh = l.dw = 0;
     if (gradients) {
@@ -1335,15 +1456,35 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
         const int w_blocks = rp == 0 ? (int)grid_for((int64_t)l.kp / BK * l.cp) : 0;
         MIXGCN_RUN_T(split_kernel, w_blocks + grid_for((int64_t)pr * l.kp / 8), H, ldh, rows, labels, meta, first, pr, l.h_rows, k,
                      l.kp, top, shift, hp, y, w_blocks, W, ldw, c, l.cp, l.w_rows, wp);
-        MIXGCN_LOGITS(logit_sums_kernel, class_tiles, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, class_tiles, sums, at_label);
-        if (l.loss_rows == 4)
-            MIXGCN_RUN(join_sums_kernel<4>, pr / 4, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
-        else
-            MIXGCN_RUN(join_sums_kernel<16>, pr / 16, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
+        if (l.one_tile) {
+            // rows of a tile: what two workgroups of a compute unit have registers and LDS for
+#define MIXGCN_ROWS(TH, TM, TN)                                                                                                          \
+    MIXGCN_RUN((logit_rows_kernel<TH, TM, TN>), pr / (64 * TN), wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, rows, losses, \
+               row_loss, l.g_rows, grads ? g : nullptr)
+            if (l.cp == kTile) {
+                if (bf16 && logit_rows == 64) MIXGCN_ROWS(1, 2, 1);
+                else if (bf16) MIXGCN_ROWS(1, 2, 4);
+                else if (logit_rows == 64) MIXGCN_ROWS(2, 2, 1);
+                else MIXGCN_ROWS(2, 2, 2);
+            } else {
+                if (bf16 && logit_rows == 64) MIXGCN_ROWS(1, 4, 1);
+                else if (bf16) MIXGCN_ROWS(1, 4, 2);
+                else MIXGCN_ROWS(2, 4, 1);
+            }
+#undef MIXGCN_ROWS
+        } else {
+            MIXGCN_LOGITS(logit_sums_kernel, class_tiles, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, class_tiles, sums,
+                          at_label);
+            if (l.loss_rows == 4)
+                MIXGCN_RUN(join_sums_kernel<4>, pr / 4, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
+            else
+                MIXGCN_RUN(join_sums_kernel<16>, pr / 16, sums, pieces, at_label, meta, first, pr, rows, norm, losses, row_loss);
+        }
         for (int q = 0; grads && q < l.col_pieces; ++q) {
             const int col0 = q * l.piece_cols;
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
-            MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
+            if (!l.one_tile)
+                MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
             Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
                             q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift, nullptr, ldd, rows};
             if (l.w_direct) ga.dW = dW;

@@ -348,3 +348,23 @@ def test_products_below_the_smallest_float(mg, c, dtype):
     torch.cuda.synchronize()
     Oracle(h, w, y).all(loss, row_loss, dh[:, :36], dw[:, :c])
     assert (dh[:, :36] != 0).any() and (dw[:, :c] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,c,share", [(1, 64, 200, 0.0), (128, 40, 256, 0.0), (257, 96, 255, 0.3), (129, 64, 128, 0.0), (3000, 130, 47, 0.2),
+                                         (20000, 128, 172, 0.9), (40001, 35, 60, 0.1), (40001, 35, 160, 0.0), (262300, 12, 150, 0.0)])
+def test_few_classes(mg, n, k, c, share, dtype):
+    """All classes in one tile, of 128 and of 256; gradients written straight to rows that start anywhere; pieces of rows."""
+    say(f"linear_xent few classes n={n} k={k} c={c} {dtype}")
+    h, w, y = inputs(n, k, c, DTYPES[dtype], seed=23, unlabelled=share)
+    loss, row_loss, dh, dw = outputs(h, w)
+    room, ws = poisoned(mg, h, c)
+    mg.linear_xent(h, w, y, loss=loss, dH=dh[:, :k], dW=dw[:, :c], row_loss=row_loss, workspace=ws)
+    again = outputs(h, w)
+    mg.linear_xent(h, w, y, loss=again[0], row_loss=again[1])
+    mg.linear_xent(h, w, y, dH=h)
+    torch.cuda.synchronize()
+    assert torch.equal(again[0], loss) and torch.equal(again[1], row_loss) and torch.equal(h, dh[:, :k])
+    h, w, y = inputs(n, k, c, DTYPES[dtype], seed=23, unlabelled=share)
+    Oracle(h, w, y).all(loss, row_loss, dh[:, :k], dw[:, :c])
+    assert (dh[:, k:] == 5).all() and (dw[:, c:] == 5).all() and (room[ws.numel():] == 255).all()
