@@ -825,8 +825,8 @@ __device__ inline void store_grad(const float (&g)[16], float minus_one, int lan
     put(o + plane, tmp + 1024, lo);
 }
 
-// planes[t], rows the listed ones and columns the classes from col0 on: 2^15 (softmax - onehot), zeros past the classes
-// and past the rows up to a whole tile.
+// planes[t], rows the listed ones and columns the classes from col0 on: 2^15 (softmax - onehot), zeros past the rows up to
+// a whole tile and past the classes up to whole blocks of 32; what blocks past these hold reaches no result.
 template <int TH, int TN>
 __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
                                                                const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
@@ -863,6 +863,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
         uint16_t* const out = planes + ((size_t)((tile.c0 + wm * 64) / BK) * g_rows + tile.r0 + (wn * TN + yy) * 32) * BK + 8 * lane;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+            if (cw + x * 32 >= c) continue;
             float g[16];
 #pragma unroll
             for (int v = 0; v < 16; ++v) g[v] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -nm.x));
@@ -888,7 +889,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
                                                                const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
                                                                const Meta* __restrict__ meta, uint32_t first, int piece_rows,
                                                                const uint32_t* __restrict__ rows, double* __restrict__ losses,
-                                                               float* __restrict__ row_loss, int g_rows, uint16_t* __restrict__ planes)
+                                                               float* __restrict__ row_loss, int g_rows, int cols, uint16_t* __restrict__ planes)
 {
     constexpr int STEP = 64 * BK * (2 * TM + TH * TN), MOST = 40960 / STEP;  // halfwords
     using P = Product<2, TH, false, false, TM, TN, MOST < 4 ? MOST : 4>;
@@ -952,7 +953,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
     if (planes) {
         float minus_one = -1.f;
         asm("" : "+v"(minus_one));
-        const size_t plane = (size_t)(64 * TM) * g_rows;
+        const size_t plane = (size_t)cols * g_rows;
 #pragma unroll
         for (int yy = 0; yy < TN; ++yy) {
             const int row = (wn * TN + yy) * 32 + (lane & 31), at = y[r0 + row] - cw;
@@ -961,6 +962,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
             uint16_t* const out = planes + ((size_t)(wm * TM) * g_rows + r0 + (wn * TN + yy) * 32) * BK + 8 * lane;
 #pragma unroll
             for (int x = 0; x < TM; ++x) {
+                if (cw + x * 32 >= c) continue;
                 float g[16];
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
@@ -1075,7 +1077,8 @@ struct GradRows {
         const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % a.row_slabs));
         const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * a.row_slabs)) * ROWS);
         const int s0 = slab * a.row_slab_cols;
-        const int s1 = s0 + a.row_slab_cols < a.piece_cols ? s0 + a.row_slab_cols : a.piece_cols;
+        const int cols = a.c - a.col0 < a.piece_cols ? (a.c - a.col0 + BK - 1) / BK * BK : a.piece_cols;
+        const int s1 = s0 + a.row_slab_cols < cols ? s0 + a.row_slab_cols : cols;
         if (a.add && s1 <= s0) return;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
         floatx16 acc[TM][TN];
@@ -1460,14 +1463,29 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             // rows of a tile: what two workgroups of a compute unit have registers and LDS for
 #define MIXGCN_ROWS(TH, TM, TN)                                                                                                          \
     MIXGCN_RUN((logit_rows_kernel<TH, TM, TN>), pr / (64 * TN), wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, rows, losses, \
-               row_loss, l.g_rows, grads ? g : nullptr)
-            if (l.cp == kTile) {
-                if (bf16 && logit_rows == 64) MIXGCN_ROWS(1, 2, 1);
+               row_loss, l.g_rows, l.cp, grads ? g : nullptr)
+            const bool few = n <= 128;
+            switch (ceil_div(c, 64)) {
+            case 1:
+                if (bf16 && few) MIXGCN_ROWS(1, 1, 1);
+                else if (bf16) MIXGCN_ROWS(1, 1, 4);
+                else if (few) MIXGCN_ROWS(2, 1, 1);
+                else MIXGCN_ROWS(2, 1, 4);
+                break;
+            case 2:
+                if (bf16 && few) MIXGCN_ROWS(1, 2, 1);
                 else if (bf16) MIXGCN_ROWS(1, 2, 4);
-                else if (logit_rows == 64) MIXGCN_ROWS(2, 2, 1);
+                else if (few) MIXGCN_ROWS(2, 2, 1);
                 else MIXGCN_ROWS(2, 2, 2);
-            } else {
-                if (bf16 && logit_rows == 64) MIXGCN_ROWS(1, 4, 1);
+                break;
+            case 3:
+                if (bf16 && few) MIXGCN_ROWS(1, 3, 1);
+                else if (bf16) MIXGCN_ROWS(1, 3, 2);
+                else if (few) MIXGCN_ROWS(2, 3, 1);
+                else MIXGCN_ROWS(2, 3, 2);
+                break;
+            default:
+                if (bf16 && few) MIXGCN_ROWS(1, 4, 1);
                 else if (bf16) MIXGCN_ROWS(1, 4, 2);
                 else MIXGCN_ROWS(2, 4, 1);
             }
