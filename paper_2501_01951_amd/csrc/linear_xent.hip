@@ -452,8 +452,8 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 // before which a wavefront waits for its own part of the step that is due and for what it has read.  LDS holds rows
 // without padding, so the 16-byte pieces of a row are put in another order, which each lane fetches from: rows of 64
 // bytes have piece p at p ^ (row / 4 % 4), and rows of the free index, in which the transposing read takes 64 bytes of
-// four rows at a time, the 64-byte block q at q ^ (row % 4) (of rows of two blocks q ^ (row / 2 % 2)).  Either way the lanes that are served together hit all
-// banks.
+// four rows at a time, the 64-byte block q at q ^ (row % 4), of rows of two or six blocks at q ^ (row / 2 % 2).  Either way
+// the lanes that are served together hit all banks.
 struct Operand {
     const uint16_t* p;  // first term of the tile's first element
     int64_t rows;       // rows of a block in memory
@@ -490,8 +490,8 @@ struct Product {
     template <int WIDTH>
     static __device__ inline int turn(int row)
     {
-        static_assert(WIDTH >= 64, "two blocks to a row at least");
-        return WIDTH == 64 ? row >> 1 & 1 : row & 3;
+        static_assert(WIDTH == 64 || WIDTH == 128 || WIDTH == 192 || WIDTH == 256, "a multiple of two or of four blocks to a row");
+        return WIDTH % 128 ? row >> 1 & 1 : row & 3;
     }
     // where lane `lane` of load `i` of a plane reads, in bytes from the plane's first element of the step
     template <bool TR, int WIDTH>
@@ -1004,7 +1004,7 @@ struct Gradients {
     int row_blocks, row_slabs, row_slab_cols;  // dH: its classes are dealt to slabs
     bool add;
     float* dh;
-    int w_slabs;                               // dW: its rows are dealt to slabs
+    int w_slabs, class_tiles;                  // dW: its rows are dealt to slabs
     float* dw;
     // where that is one slab and one block of rows, dW itself takes the sums, and dH where it is one slab and one block of classes
     float* dW;
@@ -1115,14 +1115,14 @@ struct GradRows {
     }
 };
 
-// Tiles of 64 TM features x 128 classes.
-template <int T, int TM>
+// Tiles of 64 TM features x 64 TN classes.
+template <int T, int TM, int TN>
 struct GradWeights {
-    using P = Product<T, 2, true, true, TM, 2, 2>;
+    using P = Product<T, 2, true, true, TM, TN, 2>;
 
     static __device__ inline void run(const Gradients& a, uint16_t* lds)
     {
-        const int k_tiles = a.kp / P::WA, class_tiles = a.piece_cols / kTile;
+        const int k_tiles = a.kp / P::WA, class_tiles = a.class_tiles;
         const unsigned lid = xcd_local_index(blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
         const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
         const int ct = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % class_tiles));
@@ -1131,14 +1131,14 @@ struct GradWeights {
         const int per = ((live + a.w_slabs - 1) / a.w_slabs + BK - 1) / BK * BK;
         const int r0 = slab * per, r1 = r0 + per < live ? r0 + per : live;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-        floatx16 acc[TM][2];
+        floatx16 acc[TM][TN];
         clear(acc);
         P::run({a.hp + ((size_t)(kt * P::WA / BK) * a.h_rows + r0) * BK, a.h_rows, (size_t)a.kp * a.h_rows},
-               {a.g + ((size_t)(ct * kTile / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
+               {a.g + ((size_t)(ct * P::WB / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
                r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
         if (a.dW) {
             const float inv = a.meta->count ? 1.f / (float)a.meta->count : 0.f;
-            const int f0 = kt * P::WA + wm * TM * 32, col = a.col0 + ct * kTile + wn * 64 + (lane & 31);
+            const int f0 = kt * P::WA + wm * TM * 32, col = a.col0 + ct * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
             for (int x = 0; x < TM; ++x)
 #pragma unroll
@@ -1147,27 +1147,27 @@ struct GradWeights {
                     if (f >= a.k) continue;
                     const int e = -15 - a.shift[f];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                    for (int y = 0; y < TN; ++y)
                         if (col + y * 32 < a.c) a.dW[(int64_t)f * a.ldg + col + y * 32] = ldexpf(acc[x][y][v] * inv, e);
                 }
             return;
         }
-        float* const out = a.dw + ((size_t)slab * a.kp + kt * P::WA + wm * TM * 32) * a.piece_cols + ct * kTile + wn * 64 + (lane & 31);
+        float* const out = a.dw + ((size_t)slab * a.kp + kt * P::WA + wm * TM * 32) * a.piece_cols + ct * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
         for (int x = 0; x < TM; ++x)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < TN; ++y)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
                     out[(size_t)(x * 32 + tile_row(v, lane)) * a.piece_cols + y * 32] = acc[x][y][v];
     }
 };
 
-template <int T, int TN, int TM>
+template <int T, int TN, int TM, int CN>
 __global__ __launch_bounds__(kBlock, 2) void gradients_kernel(Gradients a)
 {
     using R = GradRows<T, TN>;
-    using W = GradWeights<T, TM>;
+    using W = GradWeights<T, TM, CN>;
     __shared__ __attribute__((aligned(1024))) uint16_t lds[R::P::LDS > W::P::LDS ? R::P::LDS : W::P::LDS];
     if ((int)blockIdx.x < a.row_blocks) R::run(a, lds);
     else W::run(a, lds);
@@ -1309,7 +1309,7 @@ struct Layout {
     int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
     int w_slabs;                    // dW: rows of a piece dealt to slabs
     bool rows_direct, w_direct;     // the product writes dH, dW itself
-    int r_width, w_width;           // features of a tile of dH, of dW
+    int r_width, w_width, c_width;  // features of a tile of dH, of dW, classes of the latter
     bool one_tile;                  // all classes are in one tile of logits
     int loss_rows;                  // rows of a partial sum of the losses
     int list_step, list_blocks;
@@ -1347,13 +1347,15 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.row_pieces = (int)ceil_div(all_rows, rows);
     l.col_pieces = (int)ceil_div(l.cp, cols);
     l.r_width = l.kp % 128 ? 64 : 128;
-    l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 ? 256 : 128;
+    // up to 192 classes in one tile (262144 x 128 -> 172 fp32 398 -> 379 us, -> 47 bf16 198 -> 177)
+    l.c_width = l.one_tile && c <= 192 ? (int)up(c, 64) : kTile;
+    l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 && l.c_width <= kTile ? 256 : 128;
     // a workgroup of either gradient for every compute unit
     const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
     const int64_t s = between(1, 256 / (l.kp / l.r_width * row_tiles), col_tiles);
     l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
     l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
-    l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * col_tiles), rows / kTile);
+    l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * (l.one_tile ? ceil_div(c, l.c_width) : col_tiles)), rows / kTile);
     l.rows_direct = l.row_slabs == 1 && l.col_pieces == 1;
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
@@ -1504,16 +1506,23 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             if (!l.one_tile)
                 MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
             Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
-                            q > 0, dhp, l.w_slabs, dwp, nullptr, ldg, k, c, shift, nullptr, ldd, rows};
+                            q > 0, dhp, l.w_slabs, (int)(l.one_tile ? ceil_div(c, l.c_width) : ct), dwp, nullptr, ldg, k, c, shift, nullptr, ldd, rows};
             if (l.w_direct) ga.dW = dW;
             if (l.rows_direct) ga.dH = dH;
             if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
-            const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ct * l.w_slabs : 0);
-            if (bf16 && l.w_width == 256) MIXGCN_RUN((gradients_kernel<1, 2, 4>), grid, ga);
-            else if (bf16 && l.w_width == 128) MIXGCN_RUN((gradients_kernel<1, 2, 2>), grid, ga);
-            else if (bf16) MIXGCN_RUN((gradients_kernel<1, 1, 1>), grid, ga);
-            else if (l.w_width == 128) MIXGCN_RUN((gradients_kernel<2, 2, 2>), grid, ga);
-            else MIXGCN_RUN((gradients_kernel<2, 1, 1>), grid, ga);
+            const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ga.class_tiles * l.w_slabs : 0);
+#define MIXGCN_GRADIENTS(T, TN, TM)                                             \
+    do {                                                                        \
+        if (l.c_width == 64) MIXGCN_RUN((gradients_kernel<T, TN, TM, 1>), grid, ga);       \
+        else if (l.c_width == 128) MIXGCN_RUN((gradients_kernel<T, TN, TM, 2>), grid, ga); \
+        else MIXGCN_RUN((gradients_kernel<T, TN, TM == 4 ? 2 : TM, 3>), grid, ga); \
+    } while (0)
+            if (bf16 && l.w_width == 256) MIXGCN_GRADIENTS(1, 2, 4);
+            else if (bf16 && l.w_width == 128) MIXGCN_GRADIENTS(1, 2, 2);
+            else if (bf16) MIXGCN_GRADIENTS(1, 1, 1);
+            else if (l.w_width == 128) MIXGCN_GRADIENTS(2, 2, 2);
+            else MIXGCN_GRADIENTS(2, 1, 1);
+#undef MIXGCN_GRADIENTS
 
             const bool last = q == l.col_pieces - 1, mean = loss && last && rp == l.row_pieces - 1;
             Finish fa = {dhp, 0, l.row_slabs, pr, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
