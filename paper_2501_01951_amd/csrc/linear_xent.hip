@@ -281,23 +281,33 @@ __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H,
         }
     } else {
         b -= plan.w_blocks + plan.h_blocks;
-        const int cols = dH ? k : 0, per_row = dH ? (k + 7) / 8 : 1;
-        const int64_t items = n * per_row;
-        for (int64_t it = (int64_t)b * kBlock + tid; it < items; it += (int64_t)plan.clear_blocks * kBlock) {
-            const int64_t r = it / per_row;
-            const int j = (int)(it - r * per_row) * 8;
-            if (has_label(labels[r], c)) continue;
-            if (j == 0 && row_loss) row_loss[r] = 0.f;
-            const int64_t at = r * ldd + j;
-            if (j + 8 <= cols) {
-                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-                uint4* const o = reinterpret_cast<uint4*>((char*)dH + at * (BF16 ? 2 : 4));
-                o[0] = zero;
-                if (!BF16) o[1] = zero;
-            } else {
-                for (int e = 0; j + e < cols; ++e) {
-                    if (BF16) ((uint16_t*)dH)[at + e] = 0;
-                    else ((float*)dH)[at + e] = 0.f;
+        const int cols = dH ? k : 0, per_row = dH ? (k + 7) / 8 : 1, lanes = per_row < kBlock ? per_row : kBlock;
+        const int at_once = kBlock / lanes;
+        if (tid >= at_once * lanes) return;
+        constexpr int U = 4;
+        const int64_t step = (int64_t)plan.clear_blocks * at_once;
+        for (int64_t r0 = (int64_t)b * at_once + tid / lanes; r0 < n; r0 += U * step) {
+            int32_t y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) y[u] = r0 + u * step < n ? labels[r0 + u * step] : 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (has_label(y[u], c)) continue;
+                const int64_t r = r0 + u * step;
+                if (tid % lanes == 0 && row_loss) row_loss[r] = 0.f;
+                for (int j = 8 * (tid % lanes); j < cols; j += 8 * lanes) {
+                    const int64_t at = r * ldd + j;
+                    if (j + 8 <= cols) {
+                        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                        uint4* const o = reinterpret_cast<uint4*>((char*)dH + at * (BF16 ? 2 : 4));
+                        o[0] = zero;
+                        if (!BF16) o[1] = zero;
+                    } else {
+                        for (int e = 0; j + e < cols; ++e) {
+                            if (BF16) ((uint16_t*)dH)[at + e] = 0;
+                            else ((float*)dH)[at + e] = 0.f;
+                        }
+                    }
                 }
             }
         }
@@ -1438,7 +1448,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     tp.w_blocks = tp.w_pieces * k;
     tp.h_rows = (int)between(64, ceil_div(n, 1024), (int64_t)1 << 30);
     tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 1024);
-    tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), kBlock), 4096) : 0;
+    tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), 4 * kBlock), 2048) : 0;
     tp.alone = tp.list_blocks == 1 && tp.w_pieces == 1 && tp.h_blocks == 1;
     if (!tp.alone) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, top, 2 * l.kp);
     MIXGCN_RUN_T(top_kernel, tp.list_blocks + tp.w_blocks + tp.h_blocks + tp.clear_blocks, H, ldh, counts, rows, meta, W, ldw, k, c,
