@@ -892,7 +892,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
 }
 
 // Few classes, all in one tile: a workgroup has its rows' logits at once, and their losses and G come from one pass over them.
-// (262144 x 128 -> 172 fp32 506 -> 428 us, of 2000 x 100 -> 220 bf16 54 -> 38, of 262144 x 128 -> 47 380 -> 309.)  losses: a
+// (262144 x 128 -> 172 fp32 506 -> 400 us, 2000 x 100 -> 220 bf16 54 -> 38.)  losses: a
 // sum per 64 rows.  planes may be null.
 template <int TH, int TM, int TN>
 __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
@@ -1446,8 +1446,9 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     tp.list_step = l.list_step;
     tp.w_pieces = (int)ceil_div(c, kTopCols);
     tp.w_blocks = tp.w_pieces * k;
-    tp.h_rows = (int)between(64, ceil_div(n, 1024), (int64_t)1 << 30);
-    tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 1024);
+    // (the blocks' atomics meet in a few lines: 262144 x 128 fp32, a tenth labelled, 97 us with 1024 blocks, 94 with 512, 101 with 256)
+    tp.h_rows = (int)between(64, ceil_div(n, 512), (int64_t)1 << 30);
+    tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 512);
     tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), 4 * kBlock), 2048) : 0;
     tp.alone = tp.list_blocks == 1 && tp.w_pieces == 1 && tp.h_blocks == 1;
     if (!tp.alone) MIXGCN_RUN(count_labels_kernel, l.list_blocks, labels, n, c, l.list_step, counts, top, 2 * l.kp);
