@@ -1357,9 +1357,11 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.row_pieces = (int)ceil_div(all_rows, rows);
     l.col_pieces = (int)ceil_div(l.cp, cols);
     l.r_width = l.kp % 128 ? 64 : 128;
-    // up to 192 classes in one tile (262144 x 128 -> 172 fp32 398 -> 379 us, -> 47 bf16 198 -> 177)
+    // dW: up to 192 classes in one tile (262144 x 128 -> 172 fp32 398 -> 379 us, -> 47 bf16 198 -> 177)
     l.c_width = l.one_tile && c <= 192 ? (int)up(c, 64) : kTile;
-    l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 && l.c_width <= kTile ? 256 : 128;
+    // tiles of 256 features where the rows make slabs long (2000 x 256 -> 5000 bf16 with them 118 us, without 105; 30000 x 256 -> 2000
+    // 306, 329)
+    l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 && n > 2048 && l.c_width <= kTile ? 256 : 128;
     // a workgroup of either gradient for every compute unit
     const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
     const int64_t s = between(1, 256 / (l.kp / l.r_width * row_tiles), col_tiles);
@@ -1456,9 +1458,10 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
                  l.kp, tp, top, labels, n, dH, ldd, row_loss);
     const int nk = (int)ceil_div(k, BK), class_tiles = l.cp / kTile, pr = l.piece_rows;
     const int pieces = l.cp / kHalfTile;
-    // rows of a tile of logits: few of them for few rows, as many as the registers hold for bf16 features, whose one
-    // plane is read from LDS for two planes of weights
-    const int logit_rows = n <= 128 ? 64 : bf16 ? 256 : 128;
+    // rows of a tile of logits: as many as the registers hold for bf16 features, whose one plane is read from LDS for two planes
+    // of weights; 64, with more steps on their way, where they do not fill one or that leaves 128 tiles or less for the compute units
+    // (373 x 512 -> 381 bf16 75 -> 53 us, 300 x 100 -> 5000 fp32 53 -> 49; with 256 tiles 10007 x 256 -> 600 bf16 90 -> 93)
+    const int logit_rows = n <= 128 || (int64_t)class_tiles * ceil_div(n, bf16 ? 256 : 128) <= 128 ? 64 : bf16 ? 256 : 128;
 #define MIXGCN_LOGITS(KERNEL, CLASS_TILES, ...)                                                         \
     do {                                                                                                \
         const int64_t grid = (int64_t)(CLASS_TILES) * (pr / logit_rows);                                \
@@ -1477,8 +1480,10 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
 #define MIXGCN_ROWS(TH, TM, TN)                                                                                                          \
     MIXGCN_RUN((logit_rows_kernel<TH, TM, TN>), pr / (64 * TN), wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, meta, first, pr, rows, losses, \
                row_loss, l.g_rows, l.cp, grads ? g : nullptr)
-            const bool few = n <= 128;
-            switch (ceil_div(c, 64)) {
+            // rows of a tile likewise (40000 x 100 -> 47 bf16 with 128 tiles 65 us, with 256 62)
+            const int tm = (int)ceil_div(c, 64);
+            const bool few = ceil_div(n, tm == 1 || (tm == 2 && bf16) ? 256 : 128) <= 256;
+            switch (tm) {
             case 1:
                 if (bf16 && few) MIXGCN_ROWS(1, 1, 1);
                 else if (bf16) MIXGCN_ROWS(1, 1, 4);
