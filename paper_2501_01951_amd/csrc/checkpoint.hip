@@ -491,10 +491,31 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
     __syncthreads();
     if (tid < WA) not_finite[tid] = 0;
     __syncthreads();
-    if (__builtin_expect(least == -128.f, 0))
-        for (int64_t r = r_begin + arow; r < r_end; r += BKS / PA)
-            for (int i = 0; i < 16; ++i)
-                if (codes[r * ldq + ka + i] == -128) not_finite[acol + i] = 1;
+    // (The row padding may hold one, too: it is looked up in vain, so the looking up reads whole 16 bytes, two rows at a time:
+    // 115712 x 72 x 296 bf16 with such padding 54 -> 30 us.)
+    if (__builtin_expect(least == -128.f, 0)) {
+        uint32_t met[4] = {};
+        constexpr int STEP = BKS / PA;
+        for (int64_t r = r_begin + arow; r < r_end; r += 2 * STEP) {
+            uint4 v[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                v[u] = *reinterpret_cast<const uint4*>(codes + (r + u * STEP < r_end ? r + u * STEP : r) * ldq + ka);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    // the top bit of each byte that is 0x80
+                    const uint32_t z = w[q] ^ 0x80808080u;
+                    met[q] |= ~(((z & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | z | 0x7F7F7F7Fu);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (met[i / 4] >> (8 * (i % 4) + 7) & 1u) not_finite[acol + i] = 1;
+    }
     __syncthreads();
 
     // D layout: lane l, register v -> row 8 (v / 4) + 4 (l / 32) + v % 4, col l % 32

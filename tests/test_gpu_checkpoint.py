@@ -284,3 +284,23 @@ def test_same_bits_streams_and_graphs(mg):
         mg.checkpoint_wgrad(mg.checkpoint_pack(x), g, eager, mask=mask)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], eager)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,m", [(37, 5, 9), (3000, 72, 150), (900, 241, 40), (5000, 130, 130)])
+def test_padding_of_the_codes_does_not_count(mg, n, k, m, dtype):
+    say(f"checkpoint_wgrad padding n={n} k={k} m={m} {dtype}")
+    codes, exps, g, mask = problem(n, k, m, DTYPES[dtype], masked=True)
+    got = []
+    for fill in (0, -128, 127):
+        wide = torch.full((n, (k + 15) // 16 * 16), fill, device="cuda", dtype=torch.int8)
+        wide[:, :k] = codes
+        got.append(torch.zeros(k, (m + 3) // 4 * 4, device="cuda")[:, :m])
+        mg.checkpoint_wgrad(mg.Checkpoint(wide[:, :k], exps), g, got[-1], mask=mask)
+    # the last column's last element is NaN, in the last row alone
+    wide[n - 1, k - 1] = -128
+    got.append(torch.zeros(k, (m + 3) // 4 * 4, device="cuda")[:, :m])
+    mg.checkpoint_wgrad(mg.Checkpoint(wide[:, :k], exps), g, got[-1], mask=mask)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    assert got[3][k - 1].isnan().all() and torch.equal(got[3][:k - 1], got[0][:k - 1])
