@@ -1019,13 +1019,39 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
 // One launch has the workgroups of both, row_blocks of dH first, so that the products of one fill the end of the other.
 // 16384 x 512 -> 50001 bf16, 13 blocks of 4096 classes: 2.34 ms, 1075 TFLOP/s, matrix cores busy 53 % of the cycles; 4096 x 256 -> 32768
 // fp32 425 us, 970.  262144 x 128 -> 172 fp32: 182 us, 3.7 TB/s of G, features and dH.
+
+// The classes of a block of G are dealt to slabs for dH, so that every compute unit has a workgroup; how many are needed
+// depends on the rows with a label that there are (12839 x 352 -> 29071 bf16, a twentieth labelled, 681 -> 318 us).  There is room
+// for the sums of `planned` slabs of all rows; 0: the product writes dH itself, in one.
+struct RowSlabs {
+    int tiles;         // of features
+    int tile_rows;
+    int cols;          // classes of a whole block of G
+    int planned, piece_rows;
+
+    __host__ __device__ int row_tiles(int live) const { return (live + tile_rows - 1) / tile_rows; }
+    __host__ __device__ int slab_cols(int live) const
+    {
+        const int rt = row_tiles(live) > 0 ? row_tiles(live) : 1, col_tiles = cols / kTile;
+        const int room = planned * piece_rows / (rt * tile_rows);  // (planned * piece_rows < 2^20)
+        int n = 256 / (tiles * rt);
+        n = n < room ? n : room;
+        n = n < col_tiles ? n : col_tiles;
+        n = n > 1 ? n : 1;
+        return (col_tiles + n - 1) / n * kTile;
+    }
+    __host__ __device__ int slabs(int live) const { return (cols + slab_cols(live) - 1) / slab_cols(live); }
+    __host__ __device__ int64_t slab_rows(int live) const { return (int64_t)row_tiles(live) * tile_rows; }
+};
+
 struct Gradients {
     const uint16_t *g, *hp, *wp;
     int kp, h_rows, w_rows, g_rows;
     const Meta* meta;
     uint32_t first;
     int piece_rows, piece_cols, col0;
-    int row_blocks, row_slabs, row_slab_cols;  // dH: its classes are dealt to slabs
+    int row_blocks;
+    RowSlabs row_slabs;
     bool add;
     float* dh;
     int w_slabs, class_tiles;                  // dW: its rows are dealt to slabs
@@ -1094,15 +1120,16 @@ struct GradRows {
     {
         const int k_tiles = a.kp / P::WB, live = rows_here(a.meta, a.first, a.piece_rows);
         const unsigned row_tiles = (unsigned)(live + ROWS - 1) / ROWS;
-        const unsigned tiles = row_tiles * (unsigned)(k_tiles * a.row_slabs);
+        const int slab_cols = a.row_slabs.slab_cols(live), slabs = a.row_slabs.slabs(live);
+        const unsigned tiles = row_tiles * (unsigned)(k_tiles * slabs);
         if (blockIdx.x >= tiles) return;
         const unsigned lid = xcd_local_index(blockIdx.x, tiles);
         const int kt = __builtin_amdgcn_readfirstlane((int)(lid % k_tiles));
-        const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % a.row_slabs));
-        const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * a.row_slabs)) * ROWS);
-        const int s0 = slab * a.row_slab_cols;
+        const int slab = __builtin_amdgcn_readfirstlane((int)(lid / k_tiles % slabs));
+        const int r0 = __builtin_amdgcn_readfirstlane((int)(lid / (k_tiles * slabs)) * ROWS);
+        const int s0 = slab * slab_cols;
         const int cols = a.c - a.col0 < a.piece_cols ? (a.c - a.col0 + BK - 1) / BK * BK : a.piece_cols;
-        const int s1 = s0 + a.row_slab_cols < cols ? s0 + a.row_slab_cols : cols;
+        const int s1 = s0 + slab_cols < cols ? s0 + slab_cols : cols;
         if (a.add && s1 <= s0) return;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
         floatx16 acc[TM][TN];
@@ -1115,7 +1142,7 @@ struct GradRows {
             return;
         }
         float* const out =
-            a.dh + ((size_t)slab * a.piece_rows + r0 + wm * TM * 32) * a.kp + kt * P::WB + wn * TN * 32 + (lane & 31);
+            a.dh + ((size_t)slab * a.row_slabs.slab_rows(live) + r0 + wm * TM * 32) * a.kp + kt * P::WB + wn * TN * 32 + (lane & 31);
 #pragma unroll
         for (int x = 0; x < TM; ++x) {
             if (r0 + (wm * TM + x) * 32 >= live) continue;
@@ -1235,7 +1262,8 @@ __device__ inline float4 sum_slabs(const float* p, size_t slab, int slabs, bool 
 // sums (w_blocks), and the mean of the losses (one more, where loss is given).
 struct Finish {
     const float* dh;
-    int row_blocks, row_slabs, piece_rows;
+    int row_blocks, piece_rows;
+    RowSlabs row_slabs;
     const uint32_t* rows;
     void* dH;
     int64_t ldd;
@@ -1259,27 +1287,31 @@ __device__ inline void finish_rows(const Finish& a)
     __shared__ float4 lds[SL][kBlock / SL];
     const int live = rows_here(a.meta, a.first, a.piece_rows);
     const int per_row = (a.k + 3) / 4;
-    const int64_t it0 = (int64_t)blockIdx.x * (kBlock / SL), it = it0 + threadIdx.x % (kBlock / SL);
-    if (it0 >= (int64_t)live * per_row) return;
-    const bool in = it < (int64_t)live * per_row;
-    const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
-    const float4 s = sum_slabs<SL>(a.dh + (size_t)i * a.kp + j, (size_t)a.piece_rows * a.kp, a.row_slabs, in, lds);
-    if (!in || threadIdx.x >= kBlock / SL) return;
     const float inv = 1.f / (float)a.meta->count;
-    const float v[4] = {s.x, s.y, s.z, s.w};
-    float o[4];
+    const int slabs = a.row_slabs.slabs(live);
+    const size_t slab = (size_t)a.row_slabs.slab_rows(live) * a.kp;
+    for (int64_t it0 = (int64_t)blockIdx.x * (kBlock / SL); it0 < (int64_t)live * per_row; it0 += (int64_t)a.row_blocks * (kBlock / SL)) {
+        const int64_t it = it0 + threadIdx.x % (kBlock / SL);
+        const bool in = it < (int64_t)live * per_row;
+        const int i = in ? (int)(it / per_row) : 0, j = in ? (int)(it - (int64_t)i * per_row) * 4 : 0;
+        const float4 s = sum_slabs<SL>(a.dh + (size_t)i * a.kp + j, slab, slabs, in, lds);
+        if (SL > 1) __syncthreads();  // before the next ones are written
+        if (!in || threadIdx.x >= kBlock / SL) continue;
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        float o[4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - a.shift[a.kp + j + b]);
-    const int64_t at = (int64_t)a.rows[a.first + i] * a.ldd + j;
-    if (BF16) {
-        const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-        if (j + 4 <= a.k) *reinterpret_cast<uint2*>((uint16_t*)a.dH + at) = make_uint2(w[0], w[1]);
-        else
-            for (int b = 0; j + b < a.k; ++b) ((uint16_t*)a.dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
-    } else {
-        if (j + 4 <= a.k) *reinterpret_cast<float4*>((float*)a.dH + at) = make_float4(o[0], o[1], o[2], o[3]);
-        else
-            for (int b = 0; j + b < a.k; ++b) ((float*)a.dH)[at + b] = o[b];
+        for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - a.shift[a.kp + j + b]);
+        const int64_t at = (int64_t)a.rows[a.first + i] * a.ldd + j;
+        if (BF16) {
+            const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+            if (j + 4 <= a.k) *reinterpret_cast<uint2*>((uint16_t*)a.dH + at) = make_uint2(w[0], w[1]);
+            else
+                for (int b = 0; j + b < a.k; ++b) ((uint16_t*)a.dH)[at + b] = (uint16_t)(w[b / 2] >> (16 * (b % 2)));
+        } else {
+            if (j + 4 <= a.k) *reinterpret_cast<float4*>((float*)a.dH + at) = make_float4(o[0], o[1], o[2], o[3]);
+            else
+                for (int b = 0; j + b < a.k; ++b) ((float*)a.dH)[at + b] = o[b];
+        }
     }
 }
 
@@ -1314,12 +1346,14 @@ __device__ inline void finish_weights(const Finish& a)
     }
 }
 
-// RL, WL: lanes that share a cell of dH and of dW, 16 where there are many slabs
-template <bool BF16, int RL, int WL>
+// WL: lanes that share a cell of dW, 16 where there are many slabs (as for dH)
+template <bool BF16, int WL>
 __global__ __launch_bounds__(kBlock) void finish_kernel(Finish a)
 {
-    if ((int)blockIdx.x < a.row_blocks) finish_rows<BF16, RL>(a);
-    else if ((int)blockIdx.x < a.row_blocks + a.w_blocks) finish_weights<WL>(a);
+    if ((int)blockIdx.x < a.row_blocks) {
+        if (a.row_slabs.slabs(rows_here(a.meta, a.first, a.piece_rows)) > 4) finish_rows<BF16, 16>(a);
+        else finish_rows<BF16, 1>(a);
+    } else if ((int)blockIdx.x < a.row_blocks + a.w_blocks) finish_weights<WL>(a);
     else mean_loss(a.losses, a.loss_rows, a.meta->count, a.loss);
 }
 
@@ -1330,7 +1364,7 @@ struct Layout {
     int h_rows, w_rows, g_rows;     // rows of a block of 32 columns of the features, the weights and G
     int piece_rows, piece_cols;     // a block of G
     int row_pieces, col_pieces;
-    int row_slabs, row_slab_cols;   // dH: classes of a piece dealt to slabs
+    RowSlabs row_slabs;             // dH: classes of a piece dealt to slabs
     int w_slabs;                    // dW: rows of a piece dealt to slabs
     bool rows_direct, w_direct;     // the product writes dH, dW itself
     int r_width, w_width, c_width;  // features of a tile of dH, of dW, classes of the latter
@@ -1379,10 +1413,10 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     // a workgroup of either gradient for every compute unit
     const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
     const int64_t s = between(1, 256 / (l.kp / l.r_width * row_tiles), col_tiles);
-    l.row_slab_cols = (int)(ceil_div(col_tiles, s) * kTile);
-    l.row_slabs = (int)ceil_div(cols, l.row_slab_cols);
+    const int planned = (int)ceil_div(col_tiles, ceil_div(col_tiles, s));
     l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * (l.one_tile ? ceil_div(c, l.c_width) : col_tiles)), rows / kTile);
-    l.rows_direct = l.row_slabs == 1 && l.col_pieces == 1;
+    l.rows_direct = planned == 1 && l.col_pieces == 1;
+    l.row_slabs = {l.kp / l.r_width, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS, (int)cols, l.rows_direct ? 0 : planned, (int)rows};
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
@@ -1408,7 +1442,7 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.g = l.dh = l.dw = 0;
     if (gradients) {
         l.g = take((size_t)2 * l.g_rows * cols * 2);
-        l.dh = take(l.rows_direct ? 0 : (size_t)l.row_slabs * rows * l.kp * 4);
+        l.dh = take(l.rows_direct ? 0 : (size_t)planned * rows * l.kp * 4);
         l.dw = take(l.w_direct ? 0 : (size_t)l.w_slabs * l.kp * cols * 4);
     }
     l.bytes = at;
@@ -1452,10 +1486,10 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
         if (bf16) MIXGCN_RUN(KERNEL<true>, GRID, __VA_ARGS__);  \
         else MIXGCN_RUN(KERNEL<false>, GRID, __VA_ARGS__);      \
     } while (0)
-#define MIXGCN_RUN_T3(KERNEL, R, W, GRID, ...)                         \
-    do {                                                               \
-        if (bf16) MIXGCN_RUN((KERNEL<true, R, W>), GRID, __VA_ARGS__); \
-        else MIXGCN_RUN((KERNEL<false, R, W>), GRID, __VA_ARGS__);     \
+#define MIXGCN_RUN_T2(KERNEL, W, GRID, ...)                         \
+    do {                                                            \
+        if (bf16) MIXGCN_RUN((KERNEL<true, W>), GRID, __VA_ARGS__); \
+        else MIXGCN_RUN((KERNEL<false, W>), GRID, __VA_ARGS__);     \
     } while (0)
     TopPlan tp;
     tp.list_blocks = l.list_blocks;
@@ -1535,11 +1569,12 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
             const int pc = l.cp - col0 < l.piece_cols ? l.cp - col0 : l.piece_cols, ct = pc / kTile;
             if (!l.one_tile)
                 MIXGCN_LOGITS(logit_grad_kernel, ct, wp, l.kp, l.w_rows, c, nk, hp, l.h_rows, y, norm, meta, first, pr, col0, l.g_rows, ct, g);
-            Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs, l.row_slab_cols,
+            Gradients ga = {g, hp, wp, l.kp, l.h_rows, l.w_rows, l.g_rows, meta, first, pr, pc, col0, 0, l.row_slabs,
                             q > 0, dhp, l.w_slabs, (int)(l.one_tile ? ceil_div(c, l.c_width) : ct), dwp, nullptr, ldg, k, c, shift, nullptr, ldd, rows};
             if (l.w_direct) ga.dW = dW;
             if (l.rows_direct) ga.dH = dH;
-            if (dH) ga.row_blocks = (int)(l.kp / l.r_width * l.row_slabs * ceil_div(pr, bf16 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS));
+            // (256 at least: fewer rows with a label have more slabs)
+            if (dH) ga.row_blocks = (int)between(256, (int64_t)l.row_slabs.tiles * l.row_slabs.slabs(pr) * l.row_slabs.row_tiles(pr), 0x7FFFFFFF);
             const int64_t grid = ga.row_blocks + (dW ? (int64_t)(l.kp / l.w_width) * ga.class_tiles * l.w_slabs : 0);
 #define MIXGCN_GRADIENTS(T, TN, TM)                                             \
     do {                                                                        \
@@ -1555,23 +1590,24 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
 #undef MIXGCN_GRADIENTS
 
             const bool last = q == l.col_pieces - 1, mean = loss && last && rp == l.row_pieces - 1;
-            Finish fa = {dhp, 0, l.row_slabs, pr, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
+            Finish fa = {dhp, 0, pr, l.row_slabs, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
                          k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
-            const bool r16 = l.row_slabs > 4, w16 = l.w_slabs > 4;
-            if (dH && last && !l.rows_direct) fa.row_blocks = (int)ceil_div((int64_t)pr * ceil_div(k, 4), r16 ? kBlock / 16 : kBlock);
+            const bool w16 = l.w_slabs > 4;
+            if (dH && last && !l.rows_direct) {
+                const int64_t cells = (int64_t)pr * ceil_div(k, 4);
+                fa.row_blocks = (int)between(between(1, ceil_div(cells, kBlock / 16), 2048), ceil_div(cells, kBlock), 0x7FFFFFFF);
+            }
             if (dW && !l.w_direct) fa.w_blocks = (int)ceil_div((int64_t)k * ceil_div(fa.cols, 4), w16 ? kBlock / 16 : kBlock);
             const int64_t blocks = (int64_t)fa.row_blocks + fa.w_blocks + (mean ? 1 : 0);
             if (blocks > 0) {
-                if (r16 && w16) MIXGCN_RUN_T3(finish_kernel, 16, 16, blocks, fa);
-                else if (r16) MIXGCN_RUN_T3(finish_kernel, 16, 1, blocks, fa);
-                else if (w16) MIXGCN_RUN_T3(finish_kernel, 1, 16, blocks, fa);
-                else MIXGCN_RUN_T3(finish_kernel, 1, 1, blocks, fa);
+                if (w16) MIXGCN_RUN_T2(finish_kernel, 16, blocks, fa);
+                else MIXGCN_RUN_T2(finish_kernel, 1, blocks, fa);
             }
         }
     }
     if (loss && !grads) MIXGCN_RUN(mean_loss_kernel, 1, losses, l.loss_rows, meta, loss);
 #undef MIXGCN_LOGITS
-#undef MIXGCN_RUN_T3
+#undef MIXGCN_RUN_T2
 #undef MIXGCN_RUN_T
 #undef MIXGCN_RUN
     MIXGCN_HIP_TRY(hipGetLastError());

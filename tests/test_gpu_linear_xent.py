@@ -368,3 +368,22 @@ def test_few_classes(mg, n, k, c, share, dtype):
     h, w, y = inputs(n, k, c, DTYPES[dtype], seed=23, unlabelled=share)
     Oracle(h, w, y).all(loss, row_loss, dh[:, :k], dw[:, :c])
     assert (dh[:, k:] == 5).all() and (dw[:, c:] == 5).all() and (room[ws.numel():] == 255).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,c,live", [(12000, 100, 9000, 1), (12000, 100, 9000, 250), (12000, 200, 9000, 3000), (20000, 40, 6000, 700),
+                                        (40000, 64, 700, 40), (9000, 130, 500, 129), (17000, 24, 12000, 16500)])
+def test_few_rows_of_many_have_a_label(mg, n, k, c, live, dtype):
+    """The launches are made for all rows, what they do is dealt out for those with a label."""
+    say(f"linear_xent {live} of n={n} k={k} c={c} {dtype}")
+    h, w, y = inputs(n, k, c, DTYPES[dtype], seed=24)
+    gen = torch.Generator(device="cuda").manual_seed(live)
+    off = torch.randperm(n, device="cuda", generator=gen)[live:]
+    y[off] = -1
+    h[off] = NAN
+    loss, row_loss, dh, dw = outputs(h, w)
+    room, ws = poisoned(mg, h, c)
+    mg.linear_xent(h, w, y, loss=loss, dH=dh[:, :k], dW=dw[:, :c], row_loss=row_loss, workspace=ws)
+    torch.cuda.synchronize()
+    Oracle(h, w, y).all(loss, row_loss, dh[:, :k], dw[:, :c])
+    assert (dh[:, k:] == 5).all() and (dw[:, c:] == 5).all() and (room[ws.numel():] == 255).all()
