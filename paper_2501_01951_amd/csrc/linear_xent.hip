@@ -12,11 +12,11 @@
 // and w_k of its row such that the largest h_k w_k of all features comes to 2^28 at least, 2^14 from either side, and a
 // feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2).  f16 numbers reach down to 2^-24 and a
 // pair of terms resolves 2^-25: an element keeps its 22 bits down to 2^-17 of its column's largest where d is 0, and is off by
-// 2^-39 of it below that.  G (between -1 and 1 before the division by N) is taken times 2^15.  dH of bf16 features, which is
-// rounded to 8 bits, takes one term of either operand.  So a bf16 call has 2 + 2 + 1 + 2 products (logits twice, dH, dW), an fp32
-// one four times 3.
+// 2^-39 of it below that.  G (between -1 and 1 before the division by N) is taken times 2^15.  So a bf16 call has 2 + 2 + 3 + 2
+// products (logits twice, dH, dW), an fp32 one four times 3.  (dH of bf16 features from one term of G and of W each, two
+// products less, was wrong by 2^-11 of its terms: a tenth of the sum where the weights of a feature are alike and G W cancels.)
 //
-// What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 5.5 ms, 1070 TFLOP/s of these products over
+// What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 7.2 ms, 1050 TFLOP/s of these products over
 // the whole call (a library f16 product of 8192^3 reaches 1074 here); 4096 x 256 -> 32768 fp32 0.89 ms, 930.  Computing the
 // logits again costs 0.20 ms there; writing and reading 4 bytes a logit instead would cost as much.  Calls of few rows and
 // few classes are a chain of launches of 3 to 10 us, most of it latency.
@@ -1066,12 +1066,13 @@ struct Gradients {
     const uint32_t* rows;
 };
 
-// Tiles of 64 TM rows x 64 TN features.  One term each (bf16 features, whose gradient is rounded to 8 bits afterwards) or two.
-template <int T, int TN>
+constexpr int kGradRows = 128;  // rows of a tile of dH
+
+// Tiles of 128 rows x 64 TN features, of `BF16` or fp32 features.
+template <bool BF16, int TN>
 struct GradRows {
-    static constexpr int TM = T == 1 ? 4 : 2, STAGES = T == 1 ? 3 : 2;
-    using P = Product<T, T, false, true, TM, TN, STAGES>;
-    static constexpr int ROWS = 64 * TM;
+    static constexpr int TM = kGradRows / 64, ROWS = kGradRows;
+    using P = Product<2, 2, false, true, TM, TN, 2>;
 
     // Rows of dH from the wavefront's sums, of features f0 on and listed rows r0 on.
     static __device__ inline void write(const Gradients& a, int r0, int live, int f0, int lane, const floatx16 (&acc)[TM][TN])
@@ -1096,7 +1097,7 @@ struct GradRows {
                 for (int v = 0; v < 16; v += 2) {
                     const float g0 = ldexpf(acc[x][y][v] * inv, e[y]), g1 = ldexpf(acc[x][y][v + 1] * inv, e[y]);
                     const int r = r0 + x * 32 + tile_row(v, lane), col = f + y * 32;
-                    if (T == 1) {
+                    if (BF16) {
                         // neighboring lanes exchange, so that each has two features of one of the rows
                         const bool odd = lane & 1;
                         const int send = __float_as_int(odd ? g0 : g1);
@@ -1217,7 +1218,7 @@ struct GradWeights {
 template <int T, int TN, int TM, int CN>
 __global__ __launch_bounds__(kBlock, 2) void gradients_kernel(Gradients a)
 {
-    using R = GradRows<T, TN>;
+    using R = GradRows<T == 1, TN>;
     using W = GradWeights<T, TM, CN>;
     __shared__ __attribute__((aligned(1024))) uint16_t lds[R::P::LDS > W::P::LDS ? R::P::LDS : W::P::LDS];
     if ((int)blockIdx.x < a.row_blocks) R::run(a, lds);
@@ -1411,12 +1412,12 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     // 306, 329)
     l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 && n > 2048 && l.c_width <= kTile ? 256 : 128;
     // a workgroup of either gradient for every compute unit
-    const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS);
+    const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, kGradRows);
     const int64_t s = between(1, 256 / (l.kp / l.r_width * row_tiles), col_tiles);
     const int planned = (int)ceil_div(col_tiles, ceil_div(col_tiles, s));
     l.w_slabs = (int)between(1, 256 / (l.kp / l.w_width * (l.one_tile ? ceil_div(c, l.c_width) : col_tiles)), rows / kTile);
     l.rows_direct = planned == 1 && l.col_pieces == 1;
-    l.row_slabs = {l.kp / l.r_width, l.terms == 1 ? GradRows<1, 2>::ROWS : GradRows<2, 2>::ROWS, (int)cols, l.rows_direct ? 0 : planned, (int)rows};
+    l.row_slabs = {l.kp / l.r_width, kGradRows, (int)cols, l.rows_direct ? 0 : planned, (int)rows};
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);

@@ -1,0 +1,85 @@
+"""How near the loss without logits and its gradients come to 64 bits where rounding shows: gradients whose terms cancel,
+losses next to zero, features and rows of very different magnitudes."""
+import pytest
+
+from parity import say
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def mg():
+    import paper_2501_01951_amd as m
+
+    m.load_library()
+    return m
+
+
+def matrix(rows, cols, dtype, fill=NAN):
+    per = 16 // torch.empty(0, dtype=dtype).element_size()
+    return torch.full((rows, (cols + per - 1) // per * per), fill, device="cuda", dtype=dtype)[:, :cols]
+
+
+def inputs(n, k, c, dtype, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed + 7 * n + 3 * k + c)
+    h, w = matrix(n, k, dtype), matrix(k, c, torch.float32)
+    h[:] = torch.randn(n, k, device="cuda", generator=gen)
+    w[:] = torch.randn(k, c, device="cuda", generator=gen) * (2.0 / k ** 0.5)
+    y = torch.randint(0, c, (n,), device="cuda", generator=gen, dtype=torch.int32)
+    return h, w, y
+
+
+def results(mg, h, w, y):
+    """loss, row_loss, dH, dW"""
+    out = (torch.full((1,), NAN, device="cuda", dtype=torch.float64), torch.full((h.shape[0],), NAN, device="cuda"),
+           matrix(*h.shape, h.dtype), matrix(*w.shape, torch.float32))
+    mg.linear_xent(h, w, y, loss=out[0], row_loss=out[1], dH=out[2], dW=out[3])
+    torch.cuda.synchronize()
+    return out
+
+
+def reference(h, w, y):
+    """losses and (softmax - onehot) / n of rows that all have a label"""
+    logp = torch.log_softmax(h.double() @ w.double(), 1)
+    at = torch.arange(h.shape[0], device="cuda")
+    g = logp.exp()
+    g[at, y.long()] -= 1
+    return -logp[at, y.long()], g / h.shape[0]
+
+
+def within(what, got, ref, off):
+    bad = ~((got.double() - ref).abs() <= off)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), ref[bad][:4].tolist(), off[bad][:4].tolist())
+
+
+def steps(terms):
+    """What a sum of products of two f16 terms each is off by, of the sum of |a| |b|: 2^-22 of either operand and the product
+    of both rests; fp32 sums of 16 terms in three products to a step, cut to 2^-23, and up to 64 pieces joined."""
+    return (3 + 3 * (terms // 16 + 1) + 64) * 2.0 ** -22
+
+
+@pytest.mark.parametrize("common", [16.0, 64.0])
+@pytest.mark.parametrize("n,k,c", [(600, 64, 700), (300, 130, 200), (2100, 256, 1500), (500, 40, 60)])
+def test_gradient_of_bf16_features_whose_weights_have_a_common_part(mg, n, k, c, common):
+    """The classes' weights of a feature are a common number, which cancels in sum G W, and a spread of 1/4 around it.  G and W
+    are fp32 numbers: what is left is off by the rounding to bf16 (2^-8) and by what 22 bits of them leave, 2^-22 of
+    their products (half a thousandth here; 11 bits would leave 2^-11).  The features are so small that the logits, and
+    with them G, are exact to 2^-21 of G."""
+    say(f"linear_xent n={n} k={k} c={c} common part {common}")
+    h, w, y = inputs(n, k, c, torch.bfloat16, 31)
+    h.mul_(2.0 ** -14)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    w.copy_(torch.randn(k, c, device="cuda", generator=gen) / 4 + common * (1 + torch.rand(k, 1, device="cuda", generator=gen)))
+    dh = results(mg, h, w, y)[2]
+    _, g = reference(h, w, y)
+    wd = w.double().t().contiguous()
+    # off in G: its logits' errors, sum |h| |w| steps, and the resolution 2^-39
+    e = (h.double().abs() @ w.double().abs()).amax(1, keepdim=True) * steps(k) + 2.0 ** -21
+    g_off = (g.abs() * 2 * e) + 2.0 ** -39 / n
+    want = g @ wd
+    within("dH", dh, want, want.abs() * 2.0 ** -8 + g_off @ wd.abs() + (g.abs() @ wd.abs()) * steps(c))
