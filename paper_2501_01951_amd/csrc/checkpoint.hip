@@ -11,6 +11,7 @@
 
 #include "gemm_bf16_tiles.h"
 #include "internal.h"
+#include "load_rules.h"
 
 namespace mixgcn {
 namespace {
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
         boff[p] = (uint32_t)(brow + p * (BKS / PB)) * (uint32_t)pg + (uint32_t)(mb * ES);
         moff[p] = (uint32_t)(brow + p * (BKS / PB)) * (uint32_t)pm + (uint32_t)(mb / 32 * 4);
     }
-    const uint32_t second = !BF16 && mb + 4 < ldg ? 16u : 0u;  // the second four columns exist where the pitch has them
+    const uint32_t second = BF16 ? 0u : (uint32_t)((second_group(mb, MD) - mb) * ES);
     struct Regs {
         uint4 a[PA], b[PB][BF16 ? 1 : 2];
         uint32_t e[PA], m[MASK ? PB : 1];

@@ -24,6 +24,7 @@
 
 #include "gemm_common.h"
 #include "internal.h"
+#include "load_rules.h"
 
 namespace mixgcn {
 namespace {
@@ -110,16 +111,16 @@ __device__ inline void list_labels(int block, int blocks, const int32_t* __restr
 // ---- scales -------------------------------------------------------------------------------------
 
 template <bool BF16>
-struct Eight {  // eight features of a row; the row's pitch holds whole 16 bytes
+struct Eight {  // eight features of a row of k; the row's pitch holds whole 16 bytes
     static constexpr int V = BF16 ? 1 : 2;
     uint4 v[V];
-    __device__ inline void load(const void* p, int64_t row_at, int j, int64_t ld)
+    __device__ inline void load(const void* p, int64_t row_at, int j, int k)
     {
         if (BF16) {
             v[0] = *reinterpret_cast<const uint4*>((const uint16_t*)p + row_at + j);
         } else {
             v[0] = *reinterpret_cast<const uint4*>((const float*)p + row_at + j);
-            v[V - 1] = *reinterpret_cast<const uint4*>((const float*)p + row_at + (j + 4 < ld ? j + 4 : j));
+            v[V - 1] = *reinterpret_cast<const uint4*>((const float*)p + row_at + second_group(j, k));
         }
     }
     __device__ inline float get(int e) const
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(kBlock) void top_kernel(const void* __restrict__ H,
                     Eight<BF16> x[U] = {};
 #pragma unroll
                     for (int u = 0; u < U; ++u)
-                        if (have[u]) x[u].load(H, (i0 + i + u * at_once) * ldh, j0 + j, ldh);
+                        if (have[u]) x[u].load(H, (i0 + i + u * at_once) * ldh, j0 + j, k);
 #pragma unroll
                     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
         float x[8] = {};
         if (in && j < k) {
             Eight<BF16> v;
-            v.load(H, (int64_t)r * ldh, j, ldh);
+            v.load(H, (int64_t)r * ldh, j, k);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (j + e < k)
