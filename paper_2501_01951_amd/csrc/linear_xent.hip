@@ -635,7 +635,10 @@ __device__ inline int rows_here(const Meta* meta, uint32_t first, int piece_rows
 
 // ---- logits -------------------------------------------------------------------------------------
 // Tiles of logits come transposed, classes x rows, so that a lane holds classes of one row: sums over the classes stay
-// in the lane, but for one exchange of its halves.  In units of log 2: t = logit * log2(e).
+// in the lane, but for one exchange of its halves.  A sum of products times a2 = alpha log2(e) is a logit in units of log 2.
+// Exponentials are of the difference from the largest sum, which is exact where it is small: the largest term of a row is
+// 1, no loss is below zero, and one next to it is off by the rounding of 1 + what is beside it.  (Products with a2 before the
+// difference round by 2^-24 of the logit, and a loss next to zero was off by that, to either side.)
 //
 // A workgroup takes 128 classes (a wavefront 64) and 64 TN rows; few rows, for which there are few workgroups, have more steps on
 // their way.  Tiles are walked in groups of 8 tiles of classes: their
@@ -663,7 +666,7 @@ struct Logits {
 
 // 16384 x 512 -> 50001 bf16 1.29 ms, 1300 TFLOP/s: matrix cores busy 69 % of the cycles, at 1.7 GHz (the clock falls under this load).
 // No bank conflicts, 11 % of the reads miss the L2s.  4096 x 256 -> 32768 fp32 220 us, 940.
-// sums[piece of 64 classes][row] = { largest t, sum of 2^(t - largest) }; at_label[row] = t of the row's label.
+// sums[piece of 64 classes][row] = { largest sum of products, sum of 2^(a2 (each less the largest)) }; at_label[row]: that of the row's label.
 template <int TH, int TN>
 __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
                                                                const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
@@ -699,15 +702,14 @@ __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* _
 #pragma unroll
             for (int v = 0; v < 16; ++v) most = fmaxf(most, acc[x][yy][v]);
         most = fmaxf(most, __shfl_xor(most, 32, kWave));
-        const float top = most * a2;
-        const float base = most == -INFINITY ? 0.f : top;
+        const float base = most == -INFINITY ? 0.f : most;
         float sum = 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -base));
+            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f((acc[x][yy][v] - base) * a2);
         sum += __shfl_xor(sum, 32, kWave);
-        if (lane < 32) sums[(size_t)(cw / kHalfTile) * piece_rows + row] = make_float2(most == -INFINITY ? most : top, sum);
+        if (lane < 32) sums[(size_t)(cw / kHalfTile) * piece_rows + row] = make_float2(most, sum);
         const int at = y[row] - cw;
         if (__any(at >= 0 && at < kHalfTile)) {
             float mine = 0.f;
@@ -715,13 +717,13 @@ __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* _
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    if (at == x * 32 + tile_row(v, lane)) mine = acc[x][yy][v] * a2;
+                    if (at == x * 32 + tile_row(v, lane)) mine = acc[x][yy][v];
             if (at >= 0 && at < kHalfTile && ((at >> 2) & 1) == (lane >> 5)) at_label[row] = mine;
         }
     }
 }
 
-// A row's largest t and what its exponentials are taken times for G, from the sums of its pieces; the loss of the row.
+// A row's largest sum of products and what its exponentials are taken times for G, from the sums of its pieces; the loss of the row.
 // A block takes ROWS rows, kBlock / ROWS lanes walk the pieces of each; losses[block]: the sum of its rows' losses.
 template <int ROWS>
 __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restrict__ sums, int pieces,
@@ -737,6 +739,7 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
     const int row = blockIdx.x * ROWS + j;
     if ((int)blockIdx.x * ROWS >= live) return;
     const int rr = row < live ? row : live - 1;
+    const float a2 = meta->alpha * kLog2e;
     float top = -INFINITY, sum = 0.f;
     bool bad = false;
     for (int p0 = q; p0 < pieces; p0 += 4 * LANES) {
@@ -751,10 +754,10 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
         for (int u = 0; u < 4; ++u) {
             bad = bad || !(s[u].y == s[u].y);
             if (s[u].x > top) {
-                sum = sum * __builtin_amdgcn_exp2f(top - s[u].x) + s[u].y;
+                sum = sum * __builtin_amdgcn_exp2f((top - s[u].x) * a2) + s[u].y;
                 top = s[u].x;
             } else if (s[u].x > -INFINITY) {
-                sum += s[u].y * __builtin_amdgcn_exp2f(s[u].x - top);
+                sum += s[u].y * __builtin_amdgcn_exp2f((s[u].x - top) * a2);
             }
         }
     }
@@ -768,10 +771,10 @@ __global__ __launch_bounds__(kBlock) void join_sums_kernel(const float2* __restr
         float s = 0.f;
         // (what is not a number stays one: the lanes before it and after it add to it)
         for (int i = 0; i < LANES; ++i)
-            s += parts[i][j] * (tops[i][j] > -INFINITY ? __builtin_amdgcn_exp2f(tops[i][j] - m) : 0.f);
+            s += parts[i][j] * (tops[i][j] > -INFINITY ? __builtin_amdgcn_exp2f((tops[i][j] - m) * a2) : 0.f);
         if (!(m > -INFINITY)) s = __uint_as_float(0x7FC00000u);
         norm[row] = make_float2(m, kGradScale / s);
-        l = ((m - at_label[row]) + log2f(s)) * kLn2;
+        l = ((m - at_label[row]) * a2 + log2f(s)) * kLn2;
         if (row_loss) row_loss[rows[first + row]] = l;
     }
     __syncthreads();
@@ -889,7 +892,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
             if (cw + x * 32 >= c) continue;
             float g[16];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) g[v] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -nm.x));
+            for (int v = 0; v < 16; ++v) g[v] = __builtin_amdgcn_exp2f((acc[x][yy][v] - nm.x) * a2);
 #pragma unroll
             for (int v = 0; v < 16; ++v) g[v] *= nm.y;
             if (mark || edge)
@@ -959,13 +962,13 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
 #pragma unroll
     for (int yy = 0; yy < TN; ++yy) {
         const int row = (wn * TN + yy) * 32 + (lane & 31);
-        const float most = fmaxf(tops[0][row], tops[1][row]), base = most == -INFINITY ? 0.f : most * a2;
+        const float most = fmaxf(tops[0][row], tops[1][row]), base = most == -INFINITY ? 0.f : most;
         float sum = 0.f;
 #pragma unroll
         for (int x = 0; x < TM; ++x)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                acc[x][yy][v] = __builtin_amdgcn_exp2f(fmaf(acc[x][yy][v], a2, -base));
+                acc[x][yy][v] = __builtin_amdgcn_exp2f((acc[x][yy][v] - base) * a2);
                 sum += acc[x][yy][v];
             }
         sum += __shfl_xor(sum, 32, kWave);

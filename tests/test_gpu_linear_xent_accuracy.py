@@ -83,3 +83,28 @@ def test_gradient_of_bf16_features_whose_weights_have_a_common_part(mg, n, k, c,
     g_off = (g.abs() * 2 * e) + 2.0 ** -39 / n
     want = g @ wd
     within("dH", dh, want, want.abs() * 2.0 ** -8 + g_off @ wd.abs() + (g.abs() @ wd.abs()) * steps(c))
+
+
+@pytest.mark.parametrize("size", [1.0, 30.0, 300.0, 1500.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [50, 190, 700, 5000])
+def test_losses_of_confident_rows(mg, c, dtype, size):
+    """Logits of `size` and more, and the label the largest of them.  No loss is below zero; and one whose row has no other logit
+    within 20 of the largest is off by what the other logits' differences from it are, relative to itself, and by a rounding to
+    2^-23 of 1 + sum exp, the least of a sum of fp32 numbers, and of its logarithm."""
+    say(f"linear_xent confident rows c={c} {dtype} size {size}")
+    h, w, y = inputs(800, 64, c, DTYPES[dtype], 32)
+    w.mul_(size)
+    s = h.double() @ w.double()
+    y.copy_(s.argmax(1))
+    row_loss = results(mg, h, w, y)[1]
+    assert (row_loss >= 0).all(), row_loss.min()
+    far = s.sort(1, descending=True)[0]
+    sure = far[:, 0] - far[:, 1] > 20
+    assert size == 1.0 or sure.sum() > 20
+    want = reference(h, w, y)[0]
+    e = (h.double().abs() @ w.double().abs()).amax(1) * steps(64)
+    within("row_loss", row_loss[sure], want[sure], (want * torch.expm1(2 * e))[sure] + 2.0 ** -22)
+    # any label: a sum of exponentials that has its largest term is at least that
+    y.copy_(torch.randint(0, c, (800,), device="cuda", dtype=torch.int32))
+    assert (results(mg, h, w, y)[1] >= 0).all()
