@@ -10,7 +10,7 @@
 // the one of both rests, below 2^-22, is left out.  f16 has a narrow range, so operands are scaled by powers of two,
 // which is exact: feature k by one factor in H and another in W, chosen from the largest magnitudes h_k of its column
 // and w_k of its row such that the largest h_k w_k of all features comes to 2^28 at least, 2^14 from either side, and a
-// feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2).  f16 numbers reach down to 2^-24 and a
+// feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2), up to a d past which no logit shows it.  f16 numbers reach down to 2^-24 and a
 // pair of terms resolves 2^-25: an element keeps its 22 bits down to 2^-17 of its column's largest where d is 0, and is off by
 // 2^-39 of it below that.  G (between -1 and 1 before the division by N) is taken times 2^15.  So a bf16 call has 2 + 2 + 3 + 2
 // products (logits twice, dH, dW), an fp32 one four times 3.  (dH of bf16 features from one term of G and of W each, two
@@ -171,12 +171,18 @@ __device__ inline int most_exponent(const uint32_t* __restrict__ top, int k, int
 
 // The power of two that a feature is taken times on one side: `mine` is its largest magnitude there, `other` the one on
 // the other side.  `rest`: this side takes what is left over where their exponents cannot be shared evenly.
+// A feature whose products are below 2^-26 in a logit, and below 2^-26 of the largest, is taken for one whose products are as
+// large as that: no logit shows it, and either side, which the other one's gradient is made of, stays in the range of f16 however
+// small the other one is.  (Left to fall together a side was off by 2^-(39 - d / 2) of its largest, and 0 from d = 84.)
 __device__ inline int scale_of(uint32_t mine, uint32_t other, int most, bool rest = false)
 {
     if (!mine) return 0;
     const int e = exponent_of(mine);
     if (!other) return 14 - e;
-    const int both = e + exponent_of(other) - most, half = both >> 1;
+    const int least = -26 - (most > 0 ? most : 0);
+    int both = e + exponent_of(other) - most;
+    both = both > least ? both : least;
+    const int half = both >> 1;
     return 14 + (rest ? both - half : half) - e;
 }
 

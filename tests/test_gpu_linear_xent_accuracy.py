@@ -108,3 +108,36 @@ def test_losses_of_confident_rows(mg, c, dtype, size):
     # any label: a sum of exponentials that has its largest term is at least that
     y.copy_(torch.randint(0, c, (800,), device="cuda", dtype=torch.int32))
     assert (results(mg, h, w, y)[1] >= 0).all()
+
+
+@pytest.mark.parametrize("side", ["H", "W", "both"])
+@pytest.mark.parametrize("power", [-20, -45, -60, -80, -100, 0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [150, 400])
+def test_gradients_of_features_that_hardly_count(mg, c, dtype, power, side):
+    """Columns of H, or rows of W, next to zero (0: zero): the gradient with respect to the other operand is as large as any
+    feature's, and is off by 2^-22 of its feature's largest element (of the other operand, times the sum of |G|) beside what other
+    features' are."""
+    say(f"linear_xent c={c} {dtype} small {side} 2^{power}")
+    h, w, y = inputs(500, 40, c, DTYPES[dtype], 33)
+    factor = 2.0 ** power if power else 0.0
+    if side != "W":
+        h[:, 7] *= factor
+        h[:, 30] *= factor
+    if side != "H":
+        w[11] *= factor
+        w[30] *= factor
+    loss, row_loss, dh, dw = results(mg, h, w, y)
+    want, g = reference(h, w, y)
+    n, hd, wd = 500, h.double(), w.double()
+    e = (hd.abs() @ wd.abs()).amax(1, keepdim=True) * steps(40) + 2.0 ** -21
+    within("row_loss", row_loss, want, 2 * e[:, 0])
+    # a probability is off by twice its logits' errors, relative to itself, and by 2^-39
+    g_off, a, ht = g.abs().clamp(max=1.0 / n) * 2 * e + 2.0 ** -39 / n, g.abs(), hd.t().contiguous()
+    wt = wd.t().contiguous()
+    off = g_off @ wt.abs() + (a @ wt.abs()) * steps(c) + a.sum(1, keepdim=True) * wd.abs().amax(1) * 2.0 ** -22
+    ref = g @ wt
+    within("dH", dh, ref, off + ref.abs() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24))
+    off = ht.abs() @ g_off + (ht.abs() @ a) * steps(n) + hd.abs().amax(0)[:, None] * a.sum(0) * 2.0 ** -22
+    ref = ht @ g
+    within("dW", dw, ref, off + ref.abs() * 2.0 ** -24)
