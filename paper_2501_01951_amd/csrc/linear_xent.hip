@@ -13,7 +13,8 @@
 // feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2), up to a d past which no logit shows it.  f16 numbers reach down to 2^-24 and a
 // pair of terms resolves 2^-25: an element keeps its 22 bits down to 2^-17 of its column's largest where d is 0, and is off by
 // 2^-39 of it below that.  G (between -1 and 1 before the division by N) is taken times 2^15.  So a bf16 call has 2 + 2 + 3 + 2
-// products (logits twice, dH, dW), an fp32 one four times 3.  (dH of bf16 features from one term of G and of W each, two
+// products (logits twice, dH, dW), an fp32 one four times 3.  Where products are so large that this is not enough for rows and classes of
+// ordinary size beside them, fp32 matrix cores take the operands as they are (kMostExponent).  (dH of bf16 features from one term of G and of W each, two
 // products less, was wrong by 2^-11 of its terms: a tenth of the sum where the weights of a feature are alike and G W cancels.)
 //
 // What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 7.2 ms, 1050 TFLOP/s of these products over
@@ -35,6 +36,7 @@ typedef float floatx2v __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 typedef __attribute__((address_space(3))) uintx4 lds_uintx4;
@@ -43,14 +45,23 @@ constexpr int kTile = 128;        // classes and features of a tile
 constexpr int kMostTileRows = 256;  // rows of the largest tile
 constexpr int kHalfTile = 64;     // classes of a partial sum: what a wavefront holds
 constexpr int BK = 32;            // reduction depth of a step
-constexpr float kGradScale = 32768.f;
+constexpr int kGradShift = 15;
+constexpr float kGradScale = 32768.f;  // 2^15
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // What every kernel of a call shares, in the workspace.
 struct Meta {
     uint32_t count;  // rows that have a label
+    uint32_t wide;   // products on the fp32 matrix cores
     float alpha;     // logit = alpha * sum of the scaled products
 };
+
+// Largest exponent of a feature's largest H times its largest W at which the products run on f16 terms.  The terms are off by 2^-39 of the
+// largest of a feature, so a logit by 2^(most - 37) per feature, whatever the size of its own row: at 16 less than what fp32 sums
+// of rows of ordinary size are off by (at 22, 26, 32 and 38 losses of such rows were off by 1e-5, 3e-4, 8e-3 and 0.5).  Past it the planes hold the operands as they are, halves of fp32 numbers, and the fp32
+// matrix cores multiply them: 96 x 256 -> 32000 bf16 141 us instead of 91, 4096 x 256 -> 32768 fp32 2.41 ms instead of 0.92, 16384 x 512
+// -> 50001 bf16 31 ms instead of 7.4.
+constexpr int kMostExponent = 16;
 
 // ---- the list of rows with a label --------------------------------------------------------------
 
@@ -164,9 +175,7 @@ __device__ inline int most_exponent(const uint32_t* __restrict__ top, int k, int
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kBlock / kWave; ++w) most = most_of[w] > most ? most_of[w] : most;
-    if (most == -1000) most = 28;  // all products are zero
-    if (most > 155) most = 155;    // larger logits are not finite: alpha is
-    return most;
+    return most == -1000 ? 0 : most;  // 0: all products are zero
 }
 
 // The power of two that a feature is taken times on one side: `mine` is its largest magnitude there, `other` the one on
@@ -369,6 +378,20 @@ __device__ inline float rest_of(float x, float t)
     return fabsf(t) <= 65504.f ? r : 0.f;
 }
 
+// Eight fp32 numbers as they are: their upper halves to a plane and (bf16 numbers have none) their lower halves to the next.
+__device__ inline void put_halves(uint16_t* o, size_t plane, const float (&x)[8], bool both)
+{
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t a = __float_as_uint(x[2 * q]), b = __float_as_uint(x[2 * q + 1]);
+        hi[q] = a >> 16 | (b & 0xFFFF0000u);
+        lo[q] = (a & 0xFFFFu) | b << 16;
+    }
+    *reinterpret_cast<uint4*>(o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
 constexpr int kScaleCols = 2048;  // features whose scales a block keeps in LDS (a multiple of 8)
 
 // The two terms of eight numbers to a plane and the next.
@@ -384,8 +407,8 @@ __device__ inline void put_terms(uint16_t* o, size_t plane, const float (&x)[8],
     if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
-// planes[t]: the scaled features of the listed rows [first, first + rows of the piece), zeros past the last one up to a
-// whole tile and past the features.  y[i]: their labels, -1 past the last one.
+// planes[t]: the scaled features of the listed rows [first, first + rows of the piece) (or halves of the features themselves),
+// zeros past the last one up to a whole tile and past the features.  y[i]: their labels, -1 past the last one.
 // Bound by memory: 512 x 50001 weights and 16384 x 512 bf16 features in 61 us, 3.9 TB/s; 262144 x 128 fp32 50 us, 5.3.
 // The first w_blocks blocks: wplanes[t], the two terms of the scaled weights, rows the classes, columns the features,
 // zeros past them.
@@ -402,14 +425,18 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
     __shared__ int most_of[kBlock / kWave];
     __shared__ int16_t scale_lds[kScaleCols];
     const int most = most_exponent(top, k, kp, most_of);
+    const bool wide = most > kMostExponent;
     if (blockIdx.x == 0) {
         // for the kernels that follow
         for (int i = threadIdx.x; i < kp; i += kBlock) {
-            shift[i] = i < k ? scale_of(top[i], top[kp + i], most) : 0;
-            shift[kp + i] = i < k ? scale_of(top[kp + i], top[i], most, true) : 0;
+            shift[i] = wide ? -kGradShift : i < k ? scale_of(top[i], top[kp + i], most) : 0;
+            shift[kp + i] = wide ? -kGradShift : i < k ? scale_of(top[kp + i], top[i], most, true) : 0;
         }
         // (not down to zero, which would make NaN of the -infinity past the classes: 2^-100 already leaves all logits at zero)
-        if (threadIdx.x == 0) meta->alpha = ldexpf(1.f, most < -72 ? -100 : most - 28);
+        if (threadIdx.x == 0) {
+            meta->wide = wide;
+            meta->alpha = wide ? 1.f : ldexpf(1.f, most < -72 ? -100 : most - 28);
+        }
     }
     const bool weights = (int)blockIdx.x < w_blocks;
     for (int i = threadIdx.x; i < k && i < kScaleCols; i += kBlock)
@@ -431,10 +458,11 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int i = b * BK + 8 * q + e;
-                    const int s = i >= k ? 0 : b * BK < kScaleCols ? scale_lds[i] : scale_of(top[kp + i], top[i], most, true);
+                    const int s = i >= k || wide ? 0 : b * BK < kScaleCols ? scale_lds[i] : scale_of(top[kp + i], top[i], most, true);
                     v[e] = ldexpf(x[8 * q + e], s);
                 }
-                put_terms(o + 8 * q, plane, v, true);
+                if (wide) put_halves(o + 8 * q, plane, v, true);
+                else put_terms(o + 8 * q, plane, v, true);
             }
         }
         return;
@@ -458,9 +486,11 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (j + e < k)
-                    x[e] = ldexpf(v.get(e), j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most));
+                    x[e] = ldexpf(v.get(e), wide ? 0 : j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most));
         }
-        put_terms(planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8, plane, x, !BF16);
+        uint16_t* const o = planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8;
+        if (wide) put_halves(o, plane, x, !BF16);
+        else put_terms(o, plane, x, !BF16);
     }
 }
 
@@ -502,7 +532,11 @@ __device__ inline void load_to_lds(const uint16_t* base, uint32_t offset, uint32
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
-template <int TA, int TB, bool TRA, bool TRB, int TM, int TN, int STAGES>
+//
+// GRAD: which operand is G (0: neither).  With `wide` the planes of the other ones hold halves of fp32 numbers, G is taken
+// from its two terms, without their 2^15, and an f16 instruction over 16 reduction indices is eight fp32 ones over two, index i of either half of
+// the wavefront: a lane has the same elements of its operands for either.
+template <int TA, int TB, bool TRA, bool TRB, int TM, int TN, int STAGES, int GRAD = 0>
 struct Product {
     static constexpr int WA = 64 * TM, WB = 64 * TN;              // extents of the tile
     static constexpr int PA = WA * BK, PB = WB * BK;              // halfwords of a plane
@@ -548,8 +582,21 @@ struct Product {
         return o;
     }
 
+    // the numbers that a lane's operand stands for with `wide`
+    template <int T, bool G>
+    static __device__ inline void widen(const half8 (&f)[T], float (&o)[8])
+    {
+        ushort8 h[T];
+        __builtin_memcpy(h, f, sizeof(h));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (G) o[i] = ((float)f[0][i] + (float)f[T - 1][i]) * (1.f / kGradScale);
+            else o[i] = __uint_as_float((uint32_t)h[0][i] << 16 | (T == 2 ? (uint32_t)h[T - 1][i] : 0u));
+        }
+    }
+
     // Sums over nk steps into acc (which the caller has cleared or filled).
-    static __device__ inline void run(const Operand& a, const Operand& b, int nk, uint16_t* lds, floatx16 (&acc)[TM][TN])
+    static __device__ inline void run(const Operand& a, const Operand& b, int nk, bool wide, uint16_t* lds, floatx16 (&acc)[TM][TN])
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wm = wave / 2, wn = wave % 2;
@@ -602,20 +649,49 @@ struct Product {
                     }
             }
         };
-        clobber();
+        auto mma_wide = [&](const uint16_t* buf) {
+#pragma unroll 1
+            for (int kc = 0; kc < BK; kc += 16) {
+                float fb[TN][8];
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
-            if (s < nk) load(s, s);
-        int cur = 0;  // buffer of the step
-        for (int i = 0; i < nk; ++i) {
-            // the steps after this one that are on their way may stay so, where all of them are
-            if (i + STAGES - 2 < nk) wait_and_meet<(STAGES - 2) * LOADS>();
-            else wait_and_meet<0>();
-            const int free = cur == 0 ? STAGES - 1 : cur - 1;
-            if (i + STAGES - 1 < nk) load(i + STAGES - 1, free);
-            mma(lds + cur * BUFFER);
-            cur = cur + 1 == STAGES ? 0 : cur + 1;
-        }
+                for (int y = 0; y < TN; ++y) {
+                    half8 f[TB];
+#pragma unroll
+                    for (int t = 0; t < TB; ++t) f[t] = fragment<TRB, WB>(buf + TA * PA + t * PB, (wn * TN + y) * 32, kc, lane);
+                    widen<TB, GRAD == 2>(f, fb[y]);
+                }
+#pragma unroll
+                for (int x = 0; x < TM; ++x) {
+                    half8 f[TA];
+                    float fa[8];
+#pragma unroll
+                    for (int t = 0; t < TA; ++t) f[t] = fragment<TRA, WA>(buf + t * PA, (wm * TM + x) * 32, kc, lane);
+                    widen<TA, GRAD == 1>(f, fa);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int y = 0; y < TN; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[y][i], acc[x][y], 0, 0, 0);
+                }
+            }
+        };
+        auto walk = [&](auto multiply) {
+            clobber();
+#pragma unroll
+            for (int s = 0; s < STAGES - 1; ++s)
+                if (s < nk) load(s, s);
+            int cur = 0;  // buffer of the step
+            for (int i = 0; i < nk; ++i) {
+                // the steps after this one that are on their way may stay so, where all of them are
+                if (i + STAGES - 2 < nk) wait_and_meet<(STAGES - 2) * LOADS>();
+                else wait_and_meet<0>();
+                const int free = cur == 0 ? STAGES - 1 : cur - 1;
+                if (i + STAGES - 1 < nk) load(i + STAGES - 1, free);
+                multiply(lds + cur * BUFFER);
+                cur = cur + 1 == STAGES ? 0 : cur + 1;
+            }
+        };
+        if (__builtin_expect(wide, 0)) walk(mma_wide);
+        else walk(mma);
     }
 };
 
@@ -687,8 +763,8 @@ __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* _
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
     floatx16 acc[2][TN];
     clear(acc);
-    L::P::run({Wp + (size_t)tile.c0 * BK, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds,
-              acc);
+    L::P::run({Wp + (size_t)tile.c0 * BK, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk,
+              meta->wide, lds, acc);
     const float a2 = meta->alpha * kLog2e;
     const int cw = tile.c0 + wm * 64;
     if (cw + kHalfTile > c)  // the last classes
@@ -876,7 +952,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_grad_kernel(const uint16_t* _
     floatx16 acc[2][TN];
     clear(acc);
     L::P::run({Wp + (size_t)(col0 + tile.c0) * BK, w_rows, (size_t)kp * w_rows},
-              {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds, acc);
+              {Hp + (size_t)tile.r0 * BK, h_rows, (size_t)kp * h_rows}, nk, meta->wide, lds, acc);
     const float a2 = meta->alpha * kLog2e;
     const int cw = col0 + tile.c0 + wm * 64;
     const bool edge = cw + kHalfTile > c;
@@ -933,7 +1009,7 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
     floatx16 acc[TM][TN];
     clear(acc);
-    P::run({Wp, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)r0 * BK, h_rows, (size_t)kp * h_rows}, nk, lds, acc);
+    P::run({Wp, w_rows, (size_t)kp * w_rows}, {Hp + (size_t)r0 * BK, h_rows, (size_t)kp * h_rows}, nk, meta->wide, lds, acc);
     const float a2 = meta->alpha * kLog2e;
     uint16_t* const mine = lds + wave * 2048;
     float(*const tops)[ROWS] = reinterpret_cast<float(*)[ROWS]>(lds + 4 * 2048);  // of the two halves of the classes
@@ -1082,7 +1158,7 @@ constexpr int kGradRows = 128;  // rows of a tile of dH
 template <bool BF16, int TN>
 struct GradRows {
     static constexpr int TM = kGradRows / 64, ROWS = kGradRows;
-    using P = Product<2, 2, false, true, TM, TN, 2>;
+    using P = Product<2, 2, false, true, TM, TN, 2, 1>;
 
     // Rows of dH from the wavefront's sums, of features f0 on and listed rows r0 on.
     static __device__ inline void write(const Gradients& a, int r0, int live, int f0, int lane, const floatx16 (&acc)[TM][TN])
@@ -1091,7 +1167,7 @@ struct GradRows {
         const int f = f0 + (lane & 31);
         int e[TN];
 #pragma unroll
-        for (int y = 0; y < TN; ++y) e[y] = -15 - a.shift[a.kp + f + y * 32];
+        for (int y = 0; y < TN; ++y) e[y] = -kGradShift - a.shift[a.kp + f + y * 32];
 #pragma unroll
         for (int x = 0; x < TM; ++x) {
             if (r0 + x * 32 >= live) continue;
@@ -1147,7 +1223,7 @@ struct GradRows {
         clear(acc);
         P::run({a.g + ((size_t)(s0 / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
                {a.wp + ((size_t)(kt * P::WB / BK) * a.w_rows + a.col0 + s0) * BK, a.w_rows, (size_t)a.kp * a.w_rows},
-               s1 > s0 ? (s1 - s0) / BK : 0, lds, acc);
+               s1 > s0 ? (s1 - s0) / BK : 0, a.meta->wide, lds, acc);
         if (a.dH) {
             write(a, r0 + wm * TM * 32, live, kt * P::WB + wn * TN * 32, lane, acc);
             return;
@@ -1180,7 +1256,7 @@ struct GradRows {
 // Tiles of 64 TM features x 64 TN classes.
 template <int T, int TM, int TN>
 struct GradWeights {
-    using P = Product<T, 2, true, true, TM, TN, 2>;
+    using P = Product<T, 2, true, true, TM, TN, 2, 2>;
 
     static __device__ inline void run(const Gradients& a, uint16_t* lds)
     {
@@ -1197,7 +1273,7 @@ struct GradWeights {
         clear(acc);
         P::run({a.hp + ((size_t)(kt * P::WA / BK) * a.h_rows + r0) * BK, a.h_rows, (size_t)a.kp * a.h_rows},
                {a.g + ((size_t)(ct * P::WB / BK) * a.g_rows + r0) * BK, a.g_rows, (size_t)a.piece_cols * a.g_rows},
-               r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, lds, acc);
+               r1 > r0 ? (r1 - r0 + BK - 1) / BK : 0, a.meta->wide, lds, acc);
         if (a.dW) {
             const float inv = a.meta->count ? 1.f / (float)a.meta->count : 0.f;
             const int f0 = kt * P::WA + wm * TM * 32, col = a.col0 + ct * P::WB + wn * TN * 32 + (lane & 31);
@@ -1207,7 +1283,7 @@ struct GradWeights {
                 for (int v = 0; v < 16; ++v) {
                     const int f = f0 + x * 32 + tile_row(v, lane);
                     if (f >= a.k) continue;
-                    const int e = -15 - a.shift[f];
+                    const int e = -kGradShift - a.shift[f];
 #pragma unroll
                     for (int y = 0; y < TN; ++y)
                         if (col + y * 32 < a.c) a.dW[(int64_t)f * a.ldg + col + y * 32] = ldexpf(acc[x][y][v] * inv, e);
@@ -1311,7 +1387,7 @@ __device__ inline void finish_rows(const Finish& a)
         const float v[4] = {s.x, s.y, s.z, s.w};
         float o[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -15 - a.shift[a.kp + j + b]);
+        for (int b = 0; b < 4; ++b) o[b] = ldexpf(v[b] * inv, -kGradShift - a.shift[a.kp + j + b]);
         const int64_t at = (int64_t)a.rows[a.first + i] * a.ldd + j;
         if (BF16) {
             const uint32_t w[2] = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
@@ -1341,7 +1417,7 @@ __device__ inline void finish_weights(const Finish& a)
     const float inv = count ? 1.f / (float)count : 0.f;
     const float v[4] = {s.x, s.y, s.z, s.w};
     float* const o = a.dW + (int64_t)i * a.ldg + j;
-    const int e = -15 - a.shift[i];
+    const int e = -kGradShift - a.shift[i];
     if (j + 4 <= a.cols) {
         float4 g = make_float4(ldexpf(v[0] * inv, e), ldexpf(v[1] * inv, e), ldexpf(v[2] * inv, e), ldexpf(v[3] * inv, e));
         if (a.add) {

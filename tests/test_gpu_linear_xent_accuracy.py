@@ -141,3 +141,131 @@ def test_gradients_of_features_that_hardly_count(mg, c, dtype, power, side):
     off = ht.abs() @ g_off + (ht.abs() @ a) * steps(n) + hd.abs().amax(0)[:, None] * a.sum(0) * 2.0 ** -22
     ref = ht @ g
     within("dW", dw, ref, off + ref.abs() * 2.0 ** -24)
+
+
+# ---- rows and classes of very different magnitudes -------------------------------------------------
+
+def sum_off(terms):
+    """As steps(), or sums of fp32 products, two terms to a step, each cut to 2^-23."""
+    return max(steps(terms), (terms // 2 + 70) * 2.0 ** -23)
+
+
+def check(mg, h, w, y, dtype):
+    """Every result against 64 bits, with no allowance for what other rows or classes hold: an element of G is off by its own
+    logits' errors, the rounding of a probability, and the resolution of G; one that is 0 or 1 to the last bit by nothing."""
+    n, k = h.shape
+    c = w.shape[1]
+    loss, row_loss, dh, dw = results(mg, h, w, y)
+    want, g = reference(h, w, y)
+    hd, wd = h.double(), w.double()
+    s_off = (hd.abs() @ wd.abs()) * sum_off(k)
+    e = s_off.amax(1, keepdim=True) + 2.0 ** -22 * (1 + want[:, None])
+    within("row_loss", row_loss, want, 2 * e[:, 0])
+    within("loss", loss, want.mean().view(1), 2 * e.mean().view(1) + 1e-15)
+    p = g.clone()
+    p[torch.arange(n, device="cuda"), y.long()] += 1.0 / n
+    g_off = torch.where(g.abs() > 1e-30, (g.abs().clamp(max=1.0 / n) * torch.expm1((2 * e).clamp(max=1.0)) + p * 2.0 ** -22 + 2.0 ** -39 / n), 0.0)
+    a, ht, wt = g.abs(), hd.t().contiguous(), wd.t().contiguous()
+    ref = g @ wt
+    within("dH", dh, ref, g_off @ wt.abs() + (a @ wt.abs()) * sum_off(c) + ref.abs() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24))
+    ref = ht @ g
+    within("dW", dw, ref, ht.abs() @ g_off + (ht.abs() @ a) * sum_off(n) + ref.abs() * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("label", ["largest", "any"])
+@pytest.mark.parametrize("power", [20, 24, 30, 36, 100])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [150, 700])
+def test_one_row_far_larger_than_the_others(mg, c, dtype, power, label):
+    """The others' losses and gradients are as good as without it; also dW, to which it adds nothing where its label is its
+    largest logit."""
+    say(f"linear_xent c={c} {dtype} one row 2^{power} {label}")
+    h, w, y = inputs(300, 48, c, DTYPES[dtype], 34)
+    h[17] *= 2.0 ** power
+    if label == "largest":
+        y[17] = (h[17].double() @ w.double()).argmax()
+    check(mg, h, w, y, dtype)
+
+
+@pytest.mark.parametrize("power", [20, 30, 100])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [150, 700])
+def test_one_class_far_larger_than_the_others(mg, c, dtype, power):
+    """Its logit is by far the largest of half of the rows, and by far the least of the other half, whose losses are the
+    others' alone."""
+    say(f"linear_xent c={c} {dtype} one class 2^{power}")
+    h, w, y = inputs(300, 48, c, DTYPES[dtype], 35)
+    w[:, 33] *= 2.0 ** power
+    check(mg, h, w, y, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,c", [(1, 1, 1), (1, 4, 2), (3, 128, 1000), (129, 100, 300), (64, 602, 65), (513, 257, 700), (40, 8, 9001), (2049, 32, 47),
+                                   (3000, 130, 172), (400, 20, 250), (2500, 256, 600), (16700, 8, 8300), (140001, 8, 5), (96, 192, 1000)])
+def test_large_products_of_every_size(mg, n, k, c, dtype):
+    """Logits of 2^18 and more beside ordinary ones: tiles and pieces of every kind."""
+    say(f"linear_xent large products n={n} k={k} c={c} {dtype}")
+    h, w, y = inputs(n, k, c, DTYPES[dtype], 36)
+    h[n // 2] *= 2.0 ** 20
+    if n * c < 1 << 24:
+        check(mg, h, w, y, dtype)
+        return
+    # dW and the mean only: what the rows are is checked at the other sizes
+    loss, row_loss, dh, dw = results(mg, h, w, y)
+    e = (h.double().abs() @ w.double().abs().amax(1, keepdim=True))[:, 0] * sum_off(k) + 2.0 ** -18
+    at, ref = torch.arange(n, device="cuda"), torch.zeros(k, c, device="cuda", dtype=torch.float64)
+    for b in range(0, n, 4096):
+        want, g = reference(h[b:b + 4096], w, y[b:b + 4096])
+        within("row_loss", row_loss[b:b + 4096], want, 2 * e[b:b + 4096])
+        g *= g.shape[0] / n
+        ref += h[b:b + 4096].double().t().contiguous() @ g
+        got, dref = dh[b:b + 4096].double(), g @ w.double().t().contiguous()
+        assert (got - dref).norm() <= 4e-3 * dref.norm()
+    assert (dw.double() - ref).norm() <= 1e-4 * ref.norm()
+
+
+def test_large_products_not_finite(mg):
+    """Where products are fp32 as where they are not: a row that has an infinity or NaN has a loss and gradient that are NaN, no
+    other row has."""
+    for value in (float("inf"), -float("inf"), NAN):
+        h, w, y = inputs(260, 24, 100, torch.float32, 37)
+        h[50] *= 2.0 ** 24
+        say(f"linear_xent large products and {value}")
+        clean = results(mg, h, w, y)
+        h[133, 7] = value
+        loss, row_loss, dh, dw = results(mg, h, w, y)
+        other = torch.arange(260, device="cuda") != 133
+        assert loss.isnan().all() and row_loss[133].isnan() and dh[133].isnan().all() and dw.isnan().all()
+        assert torch.equal(row_loss[other], clean[1][other]) and torch.equal(dh[other], clean[2][other])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_graph_whose_products_become_large(mg, dtype):
+    """What the products run on is settled by what the operands hold when the graph runs."""
+    say(f"linear_xent graph of ordinary and large products {dtype}")
+    h, w, y = inputs(900, 64, 500, DTYPES[dtype], 38)
+    out = (torch.zeros(1, device="cuda", dtype=torch.float64), torch.zeros(900, device="cuda"), matrix(900, 64, h.dtype), matrix(64, 500, torch.float32))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mg.linear_xent(h, w, y, loss=out[0], row_loss=out[1], dH=out[2], dW=out[3])
+    for factor in (1.0, 2.0 ** 22, 2.0 ** -22, 2.0 ** 30):
+        h[5] *= factor
+        graph.replay()
+        eager = results(mg, h, w, y)
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+        assert torch.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_products_with_the_gradient_over_the_features(mg, dtype):
+    say(f"linear_xent large products, dH over H {dtype}")
+    for n, k, c in ((900, 40, 300), (700, 96, 120), (3000, 200, 2000)):
+        h, w, y = inputs(n, k, c, DTYPES[dtype], 39)
+        h[7] *= 2.0 ** 25
+        y[::5] = -1
+        dh, dw, again = matrix(n, k, h.dtype), matrix(k, c, torch.float32), matrix(k, c, torch.float32)
+        mg.linear_xent(h, w, y, dH=dh, dW=dw)
+        mg.linear_xent(h, w, y, dH=h, dW=again)
+        torch.cuda.synchronize()
+        assert torch.equal(h, dh) and torch.equal(dw, again) and torch.isfinite(dw).all()
