@@ -416,8 +416,9 @@ int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
  * most.  (Features whose largest H and W multiply to 2^-d of the most of all features have 2^(d/2) less of this
  * room; d counts up to 26, and as far as products of 2^-26 where the largest are above 1.)  Where the powers of two in a
  * feature's largest H and largest W multiply to 2^17 or more they run on the fp32 matrix cores instead, which takes up to
- * four times as long: no row's loss depends on how large the others are.  A probability is resolved to 2^-40.  A row whose logits are not all finite numbers has a loss and gradients that are NaN.  Outputs do
- * not overlap inputs otherwise.
+ * four times as long: no row's loss depends on how large the others are.  A probability is resolved to 2^-40.  A row has a
+ * loss and gradients that are NaN if a logit of it has a term that is not finite, or its largest is past the largest float.
+ * Outputs do not overlap inputs otherwise.
  *   workspace : device memory of mixgcn_linear_xent_workspace(...) bytes, 256-byte aligned, which the call uses
  *   until its work on the stream is done (calls that overlap need one each).  The call allocates nothing and does
  *   not synchronise.  mixgcn_linear_xent_workspace (host arithmetic; gradients: whether dH or dW is wanted) is -1

@@ -392,6 +392,10 @@ __device__ inline void put_halves(uint16_t* o, size_t plane, const float (&x)[8]
     if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
+// x, and NaN of an infinity: a logit with a term of one is not a number, also where no other term makes it one (left an infinity, a logit
+// of -infinity would leave a row's sum of exponentials a number).
+__device__ inline float number(float x) { return x + (x - x); }
+
 constexpr int kScaleCols = 2048;  // features whose scales a block keeps in LDS (a multiple of 8)
 
 // The two terms of eight numbers to a plane and the next.
@@ -459,7 +463,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
                 for (int e = 0; e < 8; ++e) {
                     const int i = b * BK + 8 * q + e;
                     const int s = i >= k || wide ? 0 : b * BK < kScaleCols ? scale_lds[i] : scale_of(top[kp + i], top[i], most, true);
-                    v[e] = ldexpf(x[8 * q + e], s);
+                    v[e] = number(ldexpf(x[8 * q + e], s));
                 }
                 if (wide) put_halves(o + 8 * q, plane, v, true);
                 else put_terms(o + 8 * q, plane, v, true);
@@ -486,7 +490,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (j + e < k)
-                    x[e] = ldexpf(v.get(e), wide ? 0 : j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most));
+                    x[e] = number(ldexpf(v.get(e), wide ? 0 : j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most)));
         }
         uint16_t* const o = planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8;
         if (wide) put_halves(o, plane, x, !BF16);

@@ -269,3 +269,36 @@ def test_large_products_with_the_gradient_over_the_features(mg, dtype):
         mg.linear_xent(h, w, y, dH=h, dW=again)
         torch.cuda.synchronize()
         assert torch.equal(h, dh) and torch.equal(dw, again) and torch.isfinite(dw).all()
+
+
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 20])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), NAN])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [1, 50, 64, 190, 700])
+def test_a_class_whose_weights_are_not_finite(mg, c, dtype, value, scale):
+    """Features that are all of one sign, or short in bits, make a logit of one infinity without a NaN on its way: a row that has one is
+    NaN all the same.  Rows of zeros have NaN logits."""
+    say(f"linear_xent c={c} {dtype} a class of {value} scale {scale}")
+    for at in {0, c // 2, c - 1}:
+        h, w, y = inputs(200, 24, c, DTYPES[dtype], 40)
+        h.abs_()
+        h.mul_(16).ceil_().mul_(scale)
+        w[:, at] = value
+        y.copy_(torch.where(y == at, (at + 1) % c, y))
+        loss, row_loss, dh, dw = results(mg, h, w, y)
+        assert loss.isnan().all() and row_loss.isnan().all() and dh.isnan().all() and dw.isnan().all()
+
+
+@pytest.mark.parametrize("c", [50, 700])
+def test_logits_past_the_largest_float(mg, c):
+    """fp32 operands that are finite and logits that are not: that row is NaN, others are as they were."""
+    say(f"linear_xent c={c} a logit past the largest float")
+    h, w, y = inputs(200, 24, c, torch.float32, 41)
+    h[9] = -(2.0 ** 100)
+    w.abs_()
+    clean = results(mg, h, w, y)
+    assert torch.isfinite(clean[1]).all()
+    h[9] = -(2.0 ** 127)
+    row_loss = results(mg, h, w, y)[1]
+    other = torch.arange(200, device="cuda") != 9
+    assert row_loss[9].isnan() and torch.equal(row_loss[other], clean[1][other])
