@@ -431,7 +431,7 @@ int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
 
 /*
  * Activations kept in 8 bits for the backward pass.  32 consecutive columns of a row share a power of two 2^s; an
- * element is code * 2^s.
+ * element is code * 2^s, or the largest finite bf16 number of its sign where that is past it (codes from 64 on, s = 122).
  *   codes     : [n_rows] x ld_codes signed bytes (16-byte aligned, ld_codes a multiple of 16), -127 .. 127.
  *   exponents : [n_rows] x ld_exponents bytes, s + 133 of columns 32 g .. 32 g + 31 at place g
  *               (ld_exponents >= ceil(n_cols / 32)).
@@ -439,7 +439,7 @@ int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
  * and rounds x / 2^s to the nearest code, ties to even: an element is off by 2^s / 2, at most 1/127 of the group's
  * largest, and the codes do not depend on anything but x.  What is not finite is left out of s and has the code
  * -128, which is read back as NaN.  Codes of the row padding up to whole 16 bytes become zero.
- * mixgcn_checkpoint_unpack writes code * 2^s, which is a bf16 number and so exact in either type; the elements of X's row
+ * mixgcn_checkpoint_unpack writes that element, which is a bf16 number and so exact in either type; the elements of X's row
  * padding up to whole 16 bytes become zero.  At most 2^28 columns.
  */
 int mixgcn_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n_rows, int32_t n_cols, int8_t* codes,

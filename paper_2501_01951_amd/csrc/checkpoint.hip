@@ -5,7 +5,8 @@
 // at most 127 (so it is 64 at least: an element is off by at most 1/127.5 of half the largest one), and -133 at
 // least.  Dividing by a power of two is exact and codes are rounded to nearest even, so the codes are the same in any
 // arithmetic; and a code times a power of two from 2^-133 up is a bf16 number: what is read back is not rounded
-// again, and enters the bf16 matrix cores as one term.  Elements that are not finite do not count for s; their code
+// again, and enters the bf16 matrix cores as one term.  (Of the largest step, 2^122, the codes from 64 on would be 2^128 and more: they
+// stand for the largest finite bf16 number, 63.75 * 2^122, which is within half a step of whatever has the code 64.)  Elements that are not finite do not count for s; their code
 // is -128, which nothing else has, and comes back as NaN.
 #include <type_traits>
 
@@ -20,6 +21,8 @@ constexpr int kGroup = 32;          // columns that share a power of two
 constexpr int kStepBias = 133;      // 2^-133 is the smallest bf16
 
 __device__ inline float step_of(uint32_t e) { return ldexpf(1.f, (int)e - kStepBias); }
+constexpr float kTopStep = 0x1p122f, kTopCode = 63.75f;  // the largest step, and the largest finite bf16 number in it
+__device__ inline float top_code(float code) { return fminf(fmaxf(code, -kTopCode), kTopCode); }
 
 template <bool BF16>
 struct Lane {
@@ -156,7 +159,11 @@ __global__ __launch_bounds__(kBlock) void pack_kernel(const void* __restrict__ X
 }
 
 // What a code stands for.
-__device__ inline float value_of(int code, float step) { return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step; }
+__device__ inline float value_of(int code, float step)
+{
+    if (code == -128) return __uint_as_float(0x7FC00000u);
+    return (step == kTopStep ? top_code((float)code) : (float)code) * step;
+}
 // What the codes of N words stand for.  (-128 is the least code, so that the least of them tells whether it is there.)
 template <int N>
 __device__ inline void values_of(const uint32_t (&w)[N], float step, float (&f)[4 * N])
@@ -167,6 +174,9 @@ __device__ inline void values_of(const uint32_t (&w)[N], float step, float (&f)[
         f[b] = (float)(int8_t)(w[b / 4] >> (8 * (b % 4)));
         least = fminf(least, f[b]);
     }
+    if (__builtin_expect(step == kTopStep, 0))
+#pragma unroll
+        for (int b = 0; b < 4 * N; ++b) f[b] = top_code(f[b]);
 #pragma unroll
     for (int b = 0; b < 4 * N; ++b) f[b] *= step;
     if (__builtin_expect(least == -128.f, 0))
@@ -534,10 +544,18 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
                 const int i = iw + x * 32 + 8 * (v / 4) + (v % 4), j = jw + y * 32;
                 if (i0 + i >= KD || j >= MD) continue;
                 const float sum = not_finite[i] ? __uint_as_float(0x7FC00000u) : acc[x][y][v] * unscale;
-                if (!BF16 && !not_finite[i]) wild = fmaf(sum, 0.f, wild);
+                if (!not_finite[i]) wild = fmaf(sum, 0.f, wild);
                 out[(size_t)i * MD + j] = sum;
             }
-    if (!BF16 && __builtin_expect(!(wild == 0.f), 0)) {
+    bool again = !(wild == 0.f);
+    if (BF16 && __builtin_expect(__syncthreads_or(again), 0)) {
+        // With one term each they are what fp32 gives, but for codes from 64 on of the largest step, which were taken for infinities.
+        bool top = false;
+        for (int64_t r = r_begin + tid; r < r_end; r += kBlock)
+            for (int q = i0 / kGroup; q * kGroup < KD && q * kGroup < i0 + WA; ++q) top = top || steps[r * lde + q] == 255;
+        again = __syncthreads_or(top) && again;
+    }
+    if (__builtin_expect(again, 0)) {
         // The lane's sums that are not finite again, as chains of fp32 multiply-adds (a term of an infinity is NaN).
         for (int c = 0; c < TM * TN * 16; ++c) {
             const int v = c % 16, i = iw + c / (16 * TN) * 32 + 8 * (v / 4) + (v % 4), j = jw + c / 16 % TN * 32;
@@ -546,7 +564,7 @@ __global__ __launch_bounds__(kBlock, 2) void wgrad_checkpoint_kernel(
             float sum = 0.f;
             for (int64_t r = r_begin; r < r_end; ++r) {
                 const float z = value_of(codes[r * ldq + i0 + i], step_of(steps[r * lde + (i0 + i) / kGroup]));
-                const float b = reinterpret_cast<const float*>(G)[r * ldg + j];
+                const float b = BF16 ? low_half(reinterpret_cast<const uint16_t*>(G)[r * ldg + j]) : reinterpret_cast<const float*>(G)[r * ldg + j];
                 const bool on = !MASK || ((mask[r * ldm + j / 32] >> (j % 32)) & 1u);
                 sum = fmaf(z, on ? b : 0.f, sum);
             }
