@@ -293,7 +293,7 @@ class GCNCheckpointStep:
     and logits do not fit: of a hidden layer the aggregate Z_l in 8 bits and the ReLU derivative as bits, and of the
     last layer nothing, whose loss and gradients come from Z and W without logits (linear_xent).  Per node and layer
     that is f_in (1 + 1/32) + f_out / 8 bytes instead of 4 (f_in + f_out) (fp32); Z, H and their gradients
-    take one pair of n x f buffers per width.  The forward products and the input gradients are those of the
+    take one buffer each of n x f per width that has them.  The forward products and the input gradients are those of the
     full-precision step; the hidden layers' weight gradients are of the 8-bit aggregates.
 
     labels: int32 [n]; a node whose label is not a class has none and takes no part in the loss.
@@ -306,11 +306,11 @@ class GCNCheckpointStep:
         self.x = padded_rows(self.n, x.shape[1], dt, dev)
         self.x.copy_(x)
         L = len(self.w)
-        widths = {w.shape[0] for w in self.w}
         # a layer's input is dead once it is aggregated, its aggregate once it is packed and multiplied: one buffer of
-        # either per width serves all layers, and their gradients on the way back
-        self.z = {f: padded_rows(self.n, f, dt, dev) for f in widths}
-        self.h = {f: padded_rows(self.n, f, dt, dev) for f in widths}
+        # either per width serves all layers, and their gradients on the way back (the first layer's input is x, which has no
+        # gradient)
+        self.z = {f: padded_rows(self.n, f, dt, dev) for f in {w.shape[0] for w in self.w}}
+        self.h = {f: padded_rows(self.n, f, dt, dev) for f in {w.shape[1] for w in self.w[:L - 1]}}
         self.kept = [B.Checkpoint.empty(self.n, w.shape[0], dev) for w in self.w[:L - 1]]
         self.positive = [torch.empty(self.n, (w.shape[1] + 31) // 32, dtype=torch.int32, device=dev) for w in self.w[:L - 1]]
         self.dw = [torch.empty_strided(w.shape, w.stride(), dtype=w.dtype, device=dev) for w in self.w]
