@@ -1681,7 +1681,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
 #undef MIXGCN_GRADIENTS
 
             const bool last = q == l.col_pieces - 1, mean = loss && last && rp == l.row_pieces - 1;
-            Finish fa = {dhp, 0, pr, l.row_slabs, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW + col0, ldg,
+            Finish fa = {dhp, 0, pr, l.row_slabs, rows, dH, ldd, dwp, 0, l.w_slabs, pc, c - col0 < pc ? c - col0 : pc, rp > 0, dW ? dW + col0 : nullptr, ldg,
                          k, l.kp, shift, meta, first, losses, l.loss_rows, loss};
             const bool w16 = l.w_slabs > 4;
             if (dH && last && !l.rows_direct) {
