@@ -392,7 +392,8 @@ int mixgcn_pipeline_window(int64_t n_nodes, int32_t n_chunks, int64_t bandwidth,
 /*
  * Loss glue (Algorithm 2, loss line): mean softmax cross-entropy over n nodes and its gradient
  * dlogits = (softmax - onehot) / n (may alias logits).  logits and dlogits are stored as
- * `dtype` (the arithmetic is fp32, the loss sum fp64).  loss: one device double.
+ * `dtype` (the arithmetic is fp32, the loss sum fp64).  loss: one device double.  A label that is not a class
+ * (0 <= label < n_classes) makes the loss NaN, and its row of dlogits that of no class.
  */
 int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_t* labels,
                         int64_t n, int32_t n_classes, void* dlogits, int64_t ldd, double* loss,

@@ -59,6 +59,9 @@ __device__ inline void st_pair(uint16_t* p, float a, float b)
     *reinterpret_cast<uint32_t*>(p) = (uint32_t)lo | ((uint32_t)hi << 16);
 }
 
+// The logit of a row's label, NaN where the label is not a class: nothing is read for it then.
+__device__ inline float of_class(int y, int c, float logit) { return (uint32_t)y < (uint32_t)c ? logit : __uint_as_float(0x7FC00000u); }
+
 // T: storage type of logits and dlogits (fp32, or bf16 widened to fp32 for the arithmetic).
 // G lanes work on one node row, two neighboring classes each (G = the power of two that covers
 // half the class count, at most 64), so a wavefront handles 64 / G rows at a time; more than 128
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(kBlock) void xent_rows_kernel(const T* logits, int6
             const float se = group_sum<G>(has ? expf(v - mx) : 0.f);
             const float lse = mx + logf(se);
             const int y = labels[rr];
-            const float xy = __shfl(v, gi * G + y, kWave);
+            const float xy = of_class(y, c, __shfl(v, gi * G + y, kWave));
             if (live) {
                 if (has) st_elem(dlogits + r * ldd + gl, (expf(v - lse) - (gl == y ? 1.f : 0.f)) * inv_n);
                 if (gl == 0) acc += (double)(lse - xy);
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(kBlock) void xent_rows_kernel(const T* logits, int6
             const float se = group_sum<G>((has0 ? expf(v0 - mx) : 0.f) + (has1 ? expf(v1 - mx) : 0.f));
             const float lse = mx + logf(se);
             const int y = labels[rr];
-            const float xy = __shfl((y & 1) ? v1 : v0, gi * G + (y >> 1), kWave);
+            const float xy = of_class(y, c, __shfl((y & 1) ? v1 : v0, gi * G + (y >> 1), kWave));
             if (live) {
                 const float p0 = (expf(v0 - lse) - (e0 == y ? 1.f : 0.f)) * inv_n;
                 const float p1 = (expf(v1 - lse) - (e0 + 1 == y ? 1.f : 0.f)) * inv_n;
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(kBlock) void xent_rows_kernel(const T* logits, int6
         se = group_sum<G>(se);
         const float lse = mx + logf(se);
         const int y = labels[rr];
-        const float xy = ld_elem(x + y);
+        const float xy = of_class(y, c, ld_elem(x + ((uint32_t)y < (uint32_t)c ? y : 0)));
         if (live) {
             for (int j = gl; j < c; j += G) {
                 const float p = expf(ld_elem(x + j) - lse);
