@@ -411,13 +411,86 @@ __device__ inline void put_terms(uint16_t* o, size_t plane, const float (&x)[8],
     if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
+// What the blocks of split_kernel share.  WIDE (the operands as they are) is a function of its own beside the terms: as a branch
+// within it made a call of one row 1.3 us longer.
+struct Split {
+    int k, kp, most;
+    const uint32_t* top;
+    const int16_t* scale;  // of the first kScaleCols features of the block's operand
+};
+
+// A thread takes 32 features of a class.
+template <bool WIDE>
+__device__ inline void split_weights(const Split& a, int w_blocks, const float* __restrict__ W, int64_t ldw, int c, int cp, int w_rows,
+                                     uint16_t* __restrict__ wplanes)
+{
+    const int64_t items = (int64_t)(a.kp / BK) * cp;
+    const size_t plane = (size_t)(a.kp / BK) * w_rows * BK;
+    for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)w_blocks * kBlock) {
+        const int b = (int)(it / cp), j = (int)(it - (int64_t)b * cp);
+        uint16_t* const o = wplanes + ((size_t)b * w_rows + j) * BK;
+        if (WIDE) {
+#pragma unroll 1
+            for (int q = 0; q < BK / 8; ++q) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = j < c && b * BK + 8 * q + e < a.k ? number(W[(int64_t)(b * BK + 8 * q + e) * ldw + j]) : 0.f;
+                put_halves(o + 8 * q, plane, v, true);
+            }
+            continue;
+        }
+        float x[BK];
+#pragma unroll
+        for (int e = 0; e < BK; ++e) x[e] = j < c && b * BK + e < a.k ? W[(int64_t)(b * BK + e) * ldw + j] : 0.f;
+#pragma unroll
+        for (int q = 0; q < BK / 8; ++q) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = b * BK + 8 * q + e;
+                const int s = i >= a.k ? 0 : b * BK < kScaleCols ? a.scale[i] : scale_of(a.top[a.kp + i], a.top[i], a.most, true);
+                v[e] = number(ldexpf(x[8 * q + e], s));
+            }
+            put_terms(o + 8 * q, plane, v, true);
+        }
+    }
+}
+
+// Four threads take the 32 features of a block in a row.
+template <bool BF16, bool WIDE>
+__device__ inline void split_rows(const Split& a, int block, int blocks, const void* __restrict__ H, int64_t ldh, const uint32_t* __restrict__ rows,
+                                  const int32_t* __restrict__ labels, int live, int h_rows, uint16_t* __restrict__ planes, int32_t* __restrict__ y)
+{
+    const int end = (live + kMostTileRows - 1) / kMostTileRows * kMostTileRows;
+    const size_t plane = (size_t)(a.kp / BK) * h_rows * BK;
+    const int64_t items = (int64_t)end * (a.kp / 8), step = (int64_t)blocks * kBlock;
+    for (int64_t it = (int64_t)block * kBlock + threadIdx.x; it < items; it += step) {
+        const int b = (int)(it / (4 * end)), at = (int)(it - (int64_t)b * (4 * end)), i = at / 4, j = b * BK + at % 4 * 8;
+        const bool in = i < live;
+        const uint32_t r = in ? rows[i] : 0u;
+        if (j == 0) y[i] = in ? labels[r] : -1;
+        float x[8] = {};
+        if (in && j < a.k) {
+            Eight<BF16> v;
+            v.load(H, (int64_t)r * ldh, j, a.k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < a.k)
+                    x[e] = number(ldexpf(v.get(e), WIDE ? 0 : j < kScaleCols ? a.scale[j + e] : scale_of(a.top[j + e], a.top[a.kp + j + e], a.most)));
+        }
+        uint16_t* const o = planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8;
+        if (WIDE) put_halves(o, plane, x, !BF16);
+        else put_terms(o, plane, x, !BF16);
+    }
+}
+
 // planes[t]: the scaled features of the listed rows [first, first + rows of the piece) (or halves of the features themselves),
 // zeros past the last one up to a whole tile and past the features.  y[i]: their labels, -1 past the last one.
 // Bound by memory: 512 x 50001 weights and 16384 x 512 bf16 features in 61 us, 3.9 TB/s; 262144 x 128 fp32 50 us, 5.3.
 // The first w_blocks blocks: wplanes[t], the two terms of the scaled weights, rows the classes, columns the features,
 // zeros past them.
 template <bool BF16>
-__global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ H, int64_t ldh,
+__global__ __launch_bounds__(kBlock, 6) void split_kernel(const void* __restrict__ H, int64_t ldh,
                                                        const uint32_t* __restrict__ rows,
                                                        const int32_t* __restrict__ labels, Meta* __restrict__ meta,
                                                        uint32_t first, int piece_rows, int h_rows, int k, int kp,
@@ -443,59 +516,19 @@ __global__ __launch_bounds__(kBlock) void split_kernel(const void* __restrict__ 
         }
     }
     const bool weights = (int)blockIdx.x < w_blocks;
+    const Split a = {k, kp, most, top, scale_lds};
+    const uint32_t count = meta->count;
+    const int live = first >= count ? 0 : count - first < (uint32_t)piece_rows ? (int)(count - first) : piece_rows;
+    if (__builtin_expect(wide, 0)) {
+        if (weights) split_weights<true>(a, w_blocks, W, ldw, c, cp, w_rows, wplanes);
+        else split_rows<BF16, true>(a, blockIdx.x - w_blocks, gridDim.x - w_blocks, H, ldh, rows + first, labels, live, h_rows, planes, y);
+        return;
+    }
     for (int i = threadIdx.x; i < k && i < kScaleCols; i += kBlock)
         scale_lds[i] = (int16_t)(weights ? scale_of(top[kp + i], top[i], most, true) : scale_of(top[i], top[kp + i], most));
     __syncthreads();
-    if (weights) {
-        // a thread takes 32 features of a class
-        const int64_t items = (int64_t)(kp / BK) * cp;
-        const size_t plane = (size_t)(kp / BK) * w_rows * BK;
-        for (int64_t it = (int64_t)blockIdx.x * kBlock + threadIdx.x; it < items; it += (int64_t)w_blocks * kBlock) {
-            const int b = (int)(it / cp), j = (int)(it - (int64_t)b * cp);
-            uint16_t* const o = wplanes + ((size_t)b * w_rows + j) * BK;
-            float x[BK];
-#pragma unroll
-            for (int e = 0; e < BK; ++e) x[e] = j < c && b * BK + e < k ? W[(int64_t)(b * BK + e) * ldw + j] : 0.f;
-#pragma unroll
-            for (int q = 0; q < BK / 8; ++q) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = b * BK + 8 * q + e;
-                    const int s = i >= k || wide ? 0 : b * BK < kScaleCols ? scale_lds[i] : scale_of(top[kp + i], top[i], most, true);
-                    v[e] = number(ldexpf(x[8 * q + e], s));
-                }
-                if (wide) put_halves(o + 8 * q, plane, v, true);
-                else put_terms(o + 8 * q, plane, v, true);
-            }
-        }
-        return;
-    }
-    const uint32_t count = meta->count;
-    if (first >= count) return;
-    const int live = count - first < (uint32_t)piece_rows ? (int)(count - first) : piece_rows;
-    const int end = (live + kMostTileRows - 1) / kMostTileRows * kMostTileRows;
-    const size_t plane = (size_t)(kp / BK) * h_rows * BK;
-    // four threads take the 32 features of a block in a row
-    const int64_t items = (int64_t)end * (kp / 8), step = (int64_t)(gridDim.x - w_blocks) * kBlock;
-    for (int64_t it = (int64_t)(blockIdx.x - w_blocks) * kBlock + threadIdx.x; it < items; it += step) {
-        const int b = (int)(it / (4 * end)), at = (int)(it - (int64_t)b * (4 * end)), i = at / 4, j = b * BK + at % 4 * 8;
-        const bool in = i < live;
-        const uint32_t r = in ? rows[first + i] : 0u;
-        if (j == 0) y[i] = in ? labels[r] : -1;
-        float x[8] = {};
-        if (in && j < k) {
-            Eight<BF16> v;
-            v.load(H, (int64_t)r * ldh, j, k);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j + e < k)
-                    x[e] = number(ldexpf(v.get(e), wide ? 0 : j < kScaleCols ? scale_lds[j + e] : scale_of(top[j + e], top[kp + j + e], most)));
-        }
-        uint16_t* const o = planes + ((size_t)b * h_rows + i) * BK + at % 4 * 8;
-        if (wide) put_halves(o, plane, x, !BF16);
-        else put_terms(o, plane, x, !BF16);
-    }
+    if (weights) split_weights<false>(a, w_blocks, W, ldw, c, cp, w_rows, wplanes);
+    else split_rows<BF16, false>(a, blockIdx.x - w_blocks, gridDim.x - w_blocks, H, ldh, rows + first, labels, live, h_rows, planes, y);
 }
 
 // ---- a tile of a product ------------------------------------------------------------------------
