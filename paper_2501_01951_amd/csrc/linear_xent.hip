@@ -17,9 +17,9 @@
 // ordinary size beside them, fp32 matrix cores take the operands as they are (kMostExponent).  (dH of bf16 features from one term of G and of W each, two
 // products less, was wrong by 2^-11 of its terms: a tenth of the sum where the weights of a feature are alike and G W cancels.)
 //
-// What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 7.2 ms, 1050 TFLOP/s of these products over
-// the whole call (a library f16 product of 8192^3 reaches 1074 here); 4096 x 256 -> 32768 fp32 0.89 ms, 930.  Computing the
-// logits again costs 0.20 ms there; writing and reading 4 bytes a logit instead would cost as much.  Calls of few rows and
+// What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 6.65 ms, 1140 TFLOP/s of these products over
+// the whole call (a library f16 product of 8192^3 reaches 1074 here); 4096 x 256 -> 32768 fp32 0.87 ms, 950.  Computing the
+// logits again costs 0.19 ms there; writing and reading 4 bytes a logit instead would cost as much.  Calls of few rows and
 // few classes are a chain of launches of 3 to 10 us, most of it latency.
 #include <type_traits>
 
@@ -59,8 +59,8 @@ struct Meta {
 // Largest exponent of a feature's largest H times its largest W at which the products run on f16 terms.  The terms are off by 2^-39 of the
 // largest of a feature, so a logit by 2^(most - 37) per feature, whatever the size of its own row: at 16 less than what fp32 sums
 // of rows of ordinary size are off by (at 22, 26, 32 and 38 losses of such rows were off by 1e-5, 3e-4, 8e-3 and 0.5).  Past it the planes hold the operands as they are, halves of fp32 numbers, and the fp32
-// matrix cores multiply them: 96 x 256 -> 32000 bf16 141 us instead of 91, 4096 x 256 -> 32768 fp32 2.41 ms instead of 0.92, 16384 x 512
-// -> 50001 bf16 31 ms instead of 7.4.
+// matrix cores multiply them: 96 x 256 -> 32000 bf16 153 us instead of 86, 4096 x 256 -> 32768 fp32 2.43 ms instead of 0.87, 16384 x 512
+// -> 50001 bf16 27 ms instead of 6.65, at 105 to 125 TFLOP/s.
 constexpr int kMostExponent = 16;
 
 // ---- the list of rows with a label --------------------------------------------------------------
@@ -486,7 +486,8 @@ __device__ inline void split_rows(const Split& a, int block, int blocks, const v
 
 // planes[t]: the scaled features of the listed rows [first, first + rows of the piece) (or halves of the features themselves),
 // zeros past the last one up to a whole tile and past the features.  y[i]: their labels, -1 past the last one.
-// Bound by memory: 512 x 50001 weights and 16384 x 512 bf16 features in 61 us, 3.9 TB/s; 262144 x 128 fp32 50 us, 5.3.
+// Bound by memory: 512 x 50001 weights and 16384 x 512 bf16 features in 70 us (two pieces of rows), 3.4 TB/s;
+// 262144 x 128 fp32 50 us, 5.3.
 // The first w_blocks blocks: wplanes[t], the two terms of the scaled weights, rows the classes, columns the features,
 // zeros past them.
 template <bool BF16>
@@ -766,7 +767,7 @@ template <int TH, int TN>
 struct Logits {
     static constexpr int STAGES = TN > 1 ? 2 : TH == 1 ? 4 : 3;
     using P = Product<2, TH, false, false, 2, TN, STAGES>;
-    static constexpr int ROWS = 64 * TN, GROUP = 8;
+    static constexpr int ROWS = 64 * TN, GROUP = 8;  // (4, 8, 16: 4096 x 256 -> 32768 fp32 879 873 885 us, 16384 x 512 -> 50001 bf16 within 0.4 %)
     int c0, r0;  // first class and row of the tile
 
     // false: no such tile.  The tiles of the rows there are, not of the grid, are dealt to the XCDs.
@@ -783,8 +784,8 @@ struct Logits {
     }
 };
 
-// 16384 x 512 -> 50001 bf16 1.29 ms, 1300 TFLOP/s: matrix cores busy 69 % of the cycles, at 1.7 GHz (the clock falls under this load).
-// No bank conflicts, 11 % of the reads miss the L2s.  4096 x 256 -> 32768 fp32 220 us, 940.
+// 16384 x 512 -> 50001 bf16 1.26 ms, 1330 TFLOP/s: matrix cores busy 67 % of the cycles, at 1.7 GHz (the clock falls under this load).
+// No bank conflicts, 11 % of the reads miss the L2s.  4096 x 256 -> 32768 fp32 190 us, 1090.
 // sums[piece of 64 classes][row] = { largest sum of products, sum of 2^(a2 (each less the largest)) }; at_label[row]: that of the row's label.
 template <int TH, int TN>
 __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
@@ -968,8 +969,9 @@ __device__ inline void store_grad(const float (&g)[16], float minus_one, int lan
     put(o + plane, tmp + 1024, lo);
 }
 
-// The two passes over 16384 x 512 -> 50001 bf16 take 1.29 and 1.74 ms: beside its products (44 % of the cycles) this one takes
-// exponentials, terms and their way through LDS, 12 vector instructions to a logit, and writes 2 TB/s.
+// The two passes over 16384 x 512 -> 50001 bf16 take 1.26 and 1.69 ms: beside its products (41 % of the cycles) this one takes
+// exponentials, terms and their way through LDS, 13 vector instructions to a logit, and writes 2 TB/s; 15 % of its LDS cycles are
+// bank conflicts.
 // planes[t], rows the listed ones and columns the classes from col0 on: 2^15 (softmax - onehot), zeros past the rows up to
 // a whole tile and past the classes up to whole blocks of 32; what blocks past these hold reaches no result.
 template <int TH, int TN>
@@ -1140,11 +1142,11 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
 // Of a block of G (the listed rows from `first` on, the classes from col0 on):
 //   dh[slab][row][kp] (+)= G[row][classes of the slab] W'^T,     dw[slab][kp][piece_cols] = H'^T[rows of the slab] G.
 // One launch has the workgroups of both, row_blocks of dH first, so that the products of one fill the end of the other.
-// 16384 x 512 -> 50001 bf16, 13 blocks of 4096 classes: 2.34 ms, 1075 TFLOP/s, matrix cores busy 53 % of the cycles; 4096 x 256 -> 32768
-// fp32 425 us, 970.  262144 x 128 -> 172 fp32: 182 us, 3.7 TB/s of G, features and dH.
+// 16384 x 512 -> 50001 bf16, 14 blocks of 8192 classes and rows: 3.41 ms, 1230 TFLOP/s, matrix cores busy 61 % of the cycles; 4096 x 256 ->
+// 32768 fp32 373 us, 1100.  262144 x 128 -> 172 fp32: 172 us, 3.9 TB/s of G, features and dH.
 
 // The classes of a block of G are dealt to slabs for dH, so that every compute unit has a workgroup; how many are needed
-// depends on the rows with a label that there are (12839 x 352 -> 29071 bf16, a twentieth labelled, 681 -> 318 us).  There is room
+// depends on the rows with a label that there are (12839 x 352 -> 29071 bf16, a twentieth labelled, 681 -> 318 us while dH was one product).  There is room
 // for the sums of `planned` slabs of all rows; 0: the product writes dH itself, in one.
 struct RowSlabs {
     int tiles;         // of features
@@ -1509,16 +1511,19 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.kp = (int)(4 * up(k, 64) <= 3 * up(k, 128) ? up(k, 64) : up(k, 128));
     l.cp = (int)up(c, kTile);
     // G, four bytes a logit, is handed on in blocks of at most 2^26 logits, of 8192 classes and as many rows (us of
-    // 16384 x 512 -> 50001 bf16 and 72640 x 32 -> 8123 fp32, 2^24, 2^25, 2^26, 2^27: 8200 6820 5850 5550, 2430 1840 1670
-    // 1770; of 30000 x 200 -> 20000 bf16 with 4096 rows of 16384 classes 3080, 8192 of 8192 2630).  Where twice the rows
-    // are all of them they are one block (the first of these 5770 -> 5510).
+    // 16384 x 512 -> 50001 bf16 and 72640 x 32 -> 8123 fp32, 2^24, 2^25, 2^26, 2^27: 8090 7080 6780 7400, 2270 1790 1610
+    // 1740; of 30000 x 200 -> 20000 bf16 with 4096 rows of 16384 classes 3490, 8192 of 8192 3150).  Where twice the rows
+    // are all of them they are one block (in two blocks 16384 x 256 -> 50001 fp32 5440 -> 5550 us, 9000 x 64 -> 60000 bf16 1510 -> 1670;
+    // 100000 x 64 -> 1000 fp32 would gain, 444 -> 394); of many features, whose sums of dH each block of classes reads and writes,
+    // where 5/4 of them are (in two blocks 16384 x 512 -> 50001 bf16 7350 -> 6920, 12000 x 384 -> 20001 fp32 2670 -> 2580, but 9000 x 512 ->
+    // 20001 bf16 1690 -> 1770).
     const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
     int64_t cols = between(kTile, l.cp, 8192);
     // (2^18 rows at most, and 2^32 cells of dH: a launch has less than 2^32 threads)
     const int64_t most_rows = between(kMostTileRows, ((int64_t)1 << 32) / l.kp / kMostTileRows * kMostTileRows, (int64_t)1 << 18);
     int64_t rows = between(kMostTileRows, most / cols / kMostTileRows * kMostTileRows, most_rows);
     l.one_tile = l.cp <= 2 * kTile;
-    if (all_rows <= 2 * rows && !l.one_tile) rows = all_rows;
+    if (all_rows <= (l.kp <= 256 ? 2 * rows : rows + rows / 4) && !l.one_tile) rows = all_rows;
     if (all_rows < rows) rows = all_rows;
     cols = between(kTile, most / rows / kTile * kTile, l.cp);
     l.piece_rows = (int)rows;
@@ -1531,8 +1536,8 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.r_width = l.kp % 128 ? 64 : 128;
     // dW: up to 192 classes in one tile (262144 x 128 -> 172 fp32 398 -> 379 us, -> 47 bf16 198 -> 177)
     l.c_width = l.one_tile && c <= 192 ? (int)up(c, 64) : kTile;
-    // tiles of 256 features where the rows make slabs long (2000 x 256 -> 5000 bf16 with them 118 us, without 105; 30000 x 256 -> 2000
-    // 306, 329)
+    // tiles of 256 features where the rows make slabs long (2000 x 256 -> 5000 bf16 with them 128 us, without 115; 30000 x 256 -> 2000
+    // 385, 392)
     l.w_width = l.kp % 128 ? 64 : l.terms == 1 && l.kp % 256 == 0 && n > 2048 && l.c_width <= kTile ? 256 : 128;
     // a workgroup of either gradient for every compute unit
     const int64_t col_tiles = cols / kTile, row_tiles = ceil_div(rows, kGradRows);
@@ -1542,7 +1547,9 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.rows_direct = planned == 1 && l.col_pieces == 1;
     l.row_slabs = {l.kp / l.r_width, kGradRows, (int)cols, l.rows_direct ? 0 : planned, (int)rows};
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
-    l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;  // few rows: more lanes to each
+    l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;
+    // (few rows: more lanes to each.  us with 4 and 16 rows to a block: 100 x 64 -> 60000 fp32 41 46, 96 x 256 -> 32000 bf16 with gradients 86 88,
+    // 1000 x 64 -> 5000 27 26, 4096 x 64 -> 5000 40 34; 6000 x 64 -> 5000 47 42, 10007 x 256 -> 5003 bf16 81 76)
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
     size_t at = 0;
@@ -1620,7 +1627,8 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     tp.list_step = l.list_step;
     tp.w_pieces = (int)ceil_div(c, kTopCols);
     tp.w_blocks = tp.w_pieces * k;
-    // (the blocks' atomics meet in a few lines: 262144 x 128 fp32, a tenth labelled, 97 us with 1024 blocks, 94 with 512, 101 with 256)
+    // (the blocks' atomics meet in a few lines: 262144 x 128 -> 172 fp32, a tenth labelled, over one input again and again, 97 us with 1024
+    // blocks, 94 with 512, 101 with 256; with 1024, 2048 or 4096 blocks to clear 105, 104, 104)
     tp.h_rows = (int)between(64, ceil_div(n, 512), (int64_t)1 << 30);
     tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 512);
     tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), 4 * kBlock), 2048) : 0;
@@ -1632,7 +1640,7 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     const int pieces = l.cp / kHalfTile;
     // rows of a tile of logits: as many as the registers hold for bf16 features, whose one plane is read from LDS for two planes
     // of weights; 64, with more steps on their way, where they do not fill one or that leaves 128 tiles or less for the compute units
-    // (373 x 512 -> 381 bf16 75 -> 53 us, 300 x 100 -> 5000 fp32 53 -> 49; with 256 tiles 10007 x 256 -> 600 bf16 90 -> 93)
+    // (373 x 512 -> 381 bf16 78 -> 57 us, 300 x 100 -> 5000 fp32 54 -> 51; up to 256 tiles 10007 x 256 -> 600 bf16 95 either way)
     const int logit_rows = n <= 128 || (int64_t)class_tiles * ceil_div(n, bf16 ? 256 : 128) <= 128 ? 64 : bf16 ? 256 : 128;
 #define MIXGCN_LOGITS(KERNEL, CLASS_TILES, ...)                                                         \
     do {                                                                                                \
