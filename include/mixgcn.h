@@ -404,8 +404,9 @@ int mixgcn_softmax_xent(int dtype, const void* logits, int64_t ldl, const int32_
  * label (0 <= label < n_classes; any other value: a row without one),
  *   row_loss[r] = log sum_c exp S[r, c] - S[r, label],   loss = mean of it over the N rows,
  *   dH = P W^T,  dW = H^T P,  P = (softmax(S) - onehot) / N.
- * Rows without a label cost nothing, whatever they hold; their rows of dH and row_loss become zero.  Without any
- * labelled row, loss, dH and dW are zero.
+ * Rows without a label are in none of the products, whatever they hold; their rows of dH and row_loss become zero.  (The
+ * launches are those of n rows with a label; what they do is that of those there are.)  Without any labelled row, loss,
+ * dH and dW are zero.
  *   H, dH   : n x k, `dtype`.  dH may be H itself (same pointer and pitch).     W, dW : k x n_classes, fp32.
  *   labels  : [n].     row_loss : [n] fp32.     loss : one device double.
  *   loss, row_loss, dH and dW may each be NULL (at least one is wanted); without dH and dW the call is the forward
@@ -441,7 +442,8 @@ int mixgcn_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
  * largest, and the codes do not depend on anything but x.  What is not finite is left out of s and has the code
  * -128, which is read back as NaN.  Codes of the row padding up to whole 16 bytes become zero.
  * mixgcn_checkpoint_unpack writes that element, which is a bf16 number and so exact in either type; the elements of X's row
- * padding up to whole 16 bytes become zero.  At most 2^28 columns.
+ * padding up to whole 16 bytes become zero (in either case also where the matrix is columns of a wider one, whose next
+ * columns these are).  At most 2^28 columns.
  */
 int mixgcn_checkpoint_pack(int dtype, const void* X, int64_t ldx, int64_t n_rows, int32_t n_cols, int8_t* codes,
                            int64_t ld_codes, uint8_t* exponents, int64_t ld_exponents, void* stream);

@@ -595,7 +595,7 @@ def linear_xent_workspace(dtype, n: int, k: int, n_classes: int, gradients: bool
 
 def linear_xent(H, W, labels, loss=None, dH=None, dW=None, row_loss=None, workspace=None, stream=None) -> None:
     """Mean softmax cross-entropy of the linear layer H W and its gradients without the logits.  labels: int32
-    [n], a row whose label is not in [0, n_classes) has none and costs nothing.  Any of loss (float64 [1]),
+    [n], a row whose label is not in [0, n_classes) has none and is in no product.  Any of loss (float64 [1]),
     row_loss (float32 [n]), dH (like H; may be H) and dW (like W) is computed that is given.  workspace: device
     memory of linear_xent_workspace bytes to use instead of allocating it."""
     n, k = H.shape
@@ -645,7 +645,8 @@ class Checkpoint:
 
 
 def checkpoint_pack(X, kept: Checkpoint = None, stream=None) -> Checkpoint:
-    """X to 8 bits."""
+    """X to 8 bits.  Codes behind the last column up to whole 16 bytes become zero: where the codes are columns of a
+    wider matrix these are its next columns."""
     n, cols = X.shape
     dtype = _dtype_of(X)
     if kept is not None:
@@ -668,7 +669,8 @@ def checkpoint_pack(X, kept: Checkpoint = None, stream=None) -> Checkpoint:
 
 
 def checkpoint_unpack(kept: Checkpoint, X, stream=None) -> None:
-    """The values of a checkpoint into X (n x cols, float32 or bfloat16)."""
+    """The values of a checkpoint into X (n x cols, float32 or bfloat16).  Elements behind the last column up to whole 16
+    bytes become zero: where X is columns of a wider matrix these are its next columns."""
     codes, exponents = kept.codes, kept.exponents
     n, cols = codes.shape
     dtype = _dtype_of(X)

@@ -184,7 +184,7 @@ __device__ inline void values_of(const uint32_t (&w)[N], float step, float (&f)[
         for (int b = 0; b < 4 * N; ++b) f[b] = value_of((int8_t)(w[b / 4] >> (8 * (b % 4))), step);
 }
 
-// Bound by memory, 2^20 x 256 fp32 in 240 us at 5.6 TB/s, 2450000 x 100 bf16 in 150 at 5.3.
+// Bound by memory, 2^20 x 256 fp32 in 240 us at 5.6 TB/s, 2450000 x 100 bf16 in 152 at 5.2.
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void unpack_kernel(const int8_t* __restrict__ codes, int64_t ldq,
                                                         const uint8_t* __restrict__ steps, int64_t lde, int64_t n,
@@ -272,9 +272,10 @@ int64_t longest_row(int64_t ldx, int es, int64_t ldq, int64_t lde)
 // a row of 128 or 256 (64) columns the 64-byte block q is at q ^ (row % 4) (row / 2 % 2), so that the four rows that are read
 // together come from all banks.
 //
-// What bounds it: 2^20 x 256 x 256 fp32 with a mask 404 us, 1020 TFLOP/s in its three products (a library bf16 product of 8192^3
-// reaches 1154), matrix cores busy 47 % of the cycles and vector instructions, most of them the three terms, 37 %: on one
-// SIMD they take turns.  2450000 x 256 x 256 bf16 430 us, 4.4 TB/s of the 5.1 that a copy reaches; 41 and 39 %.
+// What bounds it: 2^20 x 256 x 256 fp32 with a mask 393 us (464 in the first passes of a load, while the clock is down), 1050 TFLOP/s in its
+// three products (a library bf16 product of 8192^3 reaches 1154), matrix cores busy 47 % of the cycles and vector instructions, most
+// of them the three terms, 37 %: on one SIMD they take turns.  2450000 x 256 x 256 bf16 410 us, 4.6 TB/s of the 5.1 that a copy
+// reaches; 41 and 39 %.
 // 4096 x 64 x 32: 8 us, a chain of loads, products and stores of one slab, and 3 us for the slabs' sum.
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
@@ -587,7 +588,8 @@ Slabs plan_slabs(int64_t n, int32_t k, int32_t m)
     s.nit = (int)ceil_div(k, s.wa);
     s.njt = (int)ceil_div(m, s.wb);
     // two workgroups for every compute unit, of 128 rows at least (more of them and the slabs' sums cost more than they
-    // gain); four where a slab would have more than 2^14 rows, whose sums are less exact
+    // gain); four where a slab would have more than 2^14 rows, whose sums are less exact (8500000 x 128 x 128 fp32 1083 us, with two 1073; bf16
+    // 618, 562)
     const int64_t tiles = (int64_t)s.nit * s.njt;
     s.n = ceil_div(512, tiles);
     if (ceil_div(n, s.n) > 1 << 14) s.n = ceil_div(1024, tiles);

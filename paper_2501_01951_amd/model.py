@@ -297,7 +297,9 @@ class GCNCheckpointStep:
     full-precision step; the hidden layers' weight gradients are of the 8-bit aggregates.
 
     labels: int32 [n]; a node whose label is not a class has none and takes no part in the loss.
-    For few classes GCNStep, which multiplies by a narrowing W before it aggregates, is the faster one."""
+    2^20 nodes, 2^24 edges, 256 -> 256 -> 256 -> 8000 fp32: 88 ms a step and 4.6 GB (43 ms with a tenth of the nodes labelled), GCNStep 152 ms
+    and 77 GB.  For few classes GCNStep, which multiplies by a narrowing W before it aggregates, can be the faster one: 172 classes
+    37 ms and 4.8 GB against 34 and 11.3, 2450000 nodes 100 -> 256 -> 256 -> 47 bf16 48 ms and 6.4 GB against 35 and 10.7."""
 
     def __init__(self, g: B.Graph, x, weights, labels):
         self.g, self.n, self.labels = g, x.shape[0], labels
