@@ -302,3 +302,19 @@ def test_logits_past_the_largest_float(mg, c):
     row_loss = results(mg, h, w, y)[1]
     other = torch.arange(200, device="cuda") != 9
     assert row_loss[9].isnan() and torch.equal(row_loss[other], clean[1][other])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,c", [(700, 48, 333), (700, 48, 180), (1, 100, 900)])
+def test_large_products_output_by_output(mg, n, k, c, dtype):
+    """Every output alone has the bits it has beside the others, also where no gradient is asked for."""
+    h, w, y = inputs(n, k, c, DTYPES[dtype], 42)
+    h[0] *= 2.0 ** 23
+    want = results(mg, h, w, y)
+    for i, name in enumerate(("loss", "row_loss", "dH", "dW")):
+        say(f"linear_xent large products n={n} c={c} {dtype} only {name}")
+        got = (torch.full((1,), NAN, device="cuda", dtype=torch.float64), torch.full((n,), NAN, device="cuda"), matrix(n, k, h.dtype),
+               matrix(k, c, torch.float32))[i]
+        mg.linear_xent(h, w, y, **{name: got})
+        torch.cuda.synchronize()
+        assert torch.equal(got, want[i])
