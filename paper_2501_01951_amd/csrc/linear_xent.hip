@@ -6,16 +6,18 @@
 // now with the row's sum known, and hands G on a piece of the classes at a time.
 //
 // Arithmetic.  The products run on the f16 matrix cores with fp32 sums.  An fp32 number enters as two f16 terms, the
-// rounded number and the rounded rest, 22 bits and more together; a bf16 one as one.  Of the products of two terms each
-// the one of both rests, below 2^-22, is left out.  f16 has a narrow range, so operands are scaled by powers of two,
-// which is exact: feature k by one factor in H and another in W, chosen from the largest magnitudes h_k of its column
-// and w_k of its row such that the largest h_k w_k of all features comes to 2^28 at least, 2^14 from either side, and a
-// feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2), up to a d past which no logit shows it.  f16 numbers reach down to 2^-24 and a
-// pair of terms resolves 2^-25: an element keeps its 22 bits down to 2^-17 of its column's largest where d is 0, and is off by
-// 2^-39 of it below that.  G (between -1 and 1 before the division by N) is taken times 2^15.  So a bf16 call has 2 + 2 + 3 + 2
-// products (logits twice, dH, dW), an fp32 one four times 3.  Where products are so large that this is not enough for rows and classes of
-// ordinary size beside them, fp32 matrix cores take the operands as they are (kMostExponent).  (dH of bf16 features from one term of G and of W each, two
-// products less, was wrong by 2^-11 of its terms: a tenth of the sum where the weights of a feature are alike and G W cancels.)
+// rounded number and the rounded rest, 22 bits and more together; a bf16 one as one.  Of the products of two terms
+// each the one of both rests, below 2^-22, is left out.  f16 has a narrow range, so operands are scaled by powers of
+// two, which is exact: feature k by one factor in H and another in W, chosen from the largest magnitudes h_k of its
+// column and w_k of its row such that the largest h_k w_k of all features comes to 2^28 at least, 2^14 from either
+// side, and a feature whose h_k w_k is smaller by 2^d has both sides smaller by 2^(d / 2), up to a d past which no
+// logit shows it.  f16 numbers reach down to 2^-24 and a pair of terms resolves 2^-25: an element keeps its 22 bits
+// down to 2^-17 of its column's largest where d is 0, and is off by 2^-39 of it below that.  G (between -1 and 1
+// before the division by N) is taken times 2^15.  So a bf16 call has 2 + 2 + 3 + 2 products (logits twice, dH, dW),
+// an fp32 one four times 3.  Where products are so large that this is not enough for rows and classes of ordinary
+// size beside them, fp32 matrix cores take the operands as they are (kMostExponent).  (dH of bf16 features from one
+// term of G and of W each, two products less, was wrong by 2^-11 of its terms: a tenth of the sum where the weights
+// of a feature are alike and G W cancels.)
 //
 // What bounds it: the matrix cores.  16384 x 512 -> 50001 bf16 with both gradients 6.65 ms, 1140 TFLOP/s of these products over
 // the whole call (a library f16 product of 8192^3 reaches 1074 here); 4096 x 256 -> 32768 fp32 0.87 ms, 950.  Computing the
@@ -56,11 +58,12 @@ struct Meta {
     float alpha;     // logit = alpha * sum of the scaled products
 };
 
-// Largest exponent of a feature's largest H times its largest W at which the products run on f16 terms.  The terms are off by 2^-39 of the
-// largest of a feature, so a logit by 2^(most - 37) per feature, whatever the size of its own row: at 16 less than what fp32 sums
-// of rows of ordinary size are off by (at 22, 26, 32 and 38 losses of such rows were off by 1e-5, 3e-4, 8e-3 and 0.5).  Past it the planes hold the operands as they are, halves of fp32 numbers, and the fp32
-// matrix cores multiply them: 96 x 256 -> 32000 bf16 153 us instead of 86, 4096 x 256 -> 32768 fp32 2.43 ms instead of 0.87, 16384 x 512
-// -> 50001 bf16 27 ms instead of 6.65, at 105 to 125 TFLOP/s.
+// Largest exponent of a feature's largest H times its largest W at which the products run on f16 terms.  The terms
+// are off by 2^-39 of the largest of a feature, so a logit by 2^(most - 37) per feature, whatever the size of its own
+// row: at 16 less than what fp32 sums of rows of ordinary size are off by (at 22, 26, 32 and 38 losses of such rows
+// were off by 1e-5, 3e-4, 8e-3 and 0.5).  Past it the planes hold the operands as they are, halves of fp32 numbers,
+// and the fp32 matrix cores multiply them: 96 x 256 -> 32000 bf16 153 us instead of 86, 4096 x 256 -> 32768 fp32 2.43
+// ms instead of 0.87, 16384 x 512 -> 50001 bf16 27 ms instead of 6.65, at 105 to 125 TFLOP/s.
 constexpr int kMostExponent = 16;
 
 // ---- the list of rows with a label --------------------------------------------------------------
@@ -392,8 +395,8 @@ __device__ inline void put_halves(uint16_t* o, size_t plane, const float (&x)[8]
     if (both) *reinterpret_cast<uint4*>(o + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
-// x, and NaN of an infinity: a logit with a term of one is not a number, also where no other term makes it one (left an infinity, a logit
-// of -infinity would leave a row's sum of exponentials a number).
+// x, and NaN of an infinity: a logit with a term of one is not a number, also where no other term makes it one (left
+// an infinity, a logit of -infinity would leave a row's sum of exponentials a number).
 __device__ inline float number(float x) { return x + (x - x); }
 
 constexpr int kScaleCols = 2048;  // features whose scales a block keeps in LDS (a multiple of 8)
@@ -571,9 +574,9 @@ __device__ inline void load_to_lds(const uint16_t* base, uint32_t offset, uint32
 }
 
 //
-// GRAD: which operand is G (0: neither).  With `wide` the planes of the other ones hold halves of fp32 numbers, G is taken
-// from its two terms, without their 2^15, and an f16 instruction over 16 reduction indices is eight fp32 ones over two, index i of either half of
-// the wavefront: a lane has the same elements of its operands for either.
+// GRAD: which operand is G (0: neither).  With `wide` the planes of the other ones hold halves of fp32 numbers, G is
+// taken from its two terms, without their 2^15, and an f16 instruction over 16 reduction indices is eight fp32 ones
+// over two, index i of either half of the wavefront: a lane has the same elements of its operands for either.
 template <int TA, int TB, bool TRA, bool TRB, int TM, int TN, int STAGES, int GRAD = 0>
 struct Product {
     static constexpr int WA = 64 * TM, WB = 64 * TN;              // extents of the tile
@@ -784,9 +787,10 @@ struct Logits {
     }
 };
 
-// 16384 x 512 -> 50001 bf16 1.26 ms, 1330 TFLOP/s: matrix cores busy 67 % of the cycles, at 1.7 GHz (the clock falls under this load).
-// No bank conflicts, 11 % of the reads miss the L2s.  4096 x 256 -> 32768 fp32 190 us, 1090.
-// sums[piece of 64 classes][row] = { largest sum of products, sum of 2^(a2 (each less the largest)) }; at_label[row]: that of the row's label.
+// 16384 x 512 -> 50001 bf16 1.26 ms, 1330 TFLOP/s: matrix cores busy 67 % of the cycles, at 1.7 GHz (the clock falls
+// under this load). No bank conflicts, 11 % of the reads miss the L2s.  4096 x 256 -> 32768 fp32 190 us, 1090.
+// sums[piece of 64 classes][row] = { largest sum of products, sum of 2^(a2 (each less the largest)) }; at_label[row]:
+// that of the row's label.
 template <int TH, int TN>
 __global__ __launch_bounds__(kBlock, 2) void logit_sums_kernel(const uint16_t* __restrict__ Wp, int kp, int w_rows, int c, int nk,
                                                                const uint16_t* __restrict__ Hp, int h_rows, const int32_t* __restrict__ y,
@@ -1142,12 +1146,13 @@ __global__ __launch_bounds__(kBlock, 2) void logit_rows_kernel(const uint16_t* _
 // Of a block of G (the listed rows from `first` on, the classes from col0 on):
 //   dh[slab][row][kp] (+)= G[row][classes of the slab] W'^T,     dw[slab][kp][piece_cols] = H'^T[rows of the slab] G.
 // One launch has the workgroups of both, row_blocks of dH first, so that the products of one fill the end of the other.
-// 16384 x 512 -> 50001 bf16, 14 blocks of 8192 classes and rows: 3.41 ms, 1230 TFLOP/s, matrix cores busy 61 % of the cycles; 4096 x 256 ->
-// 32768 fp32 373 us, 1100.  262144 x 128 -> 172 fp32: 172 us, 3.9 TB/s of G, features and dH.
+// 16384 x 512 -> 50001 bf16, 14 blocks of 8192 classes and rows: 3.41 ms, 1230 TFLOP/s, matrix cores busy 61 % of the
+// cycles; 4096 x 256 -> 32768 fp32 373 us, 1100.  262144 x 128 -> 172 fp32: 172 us, 3.9 TB/s of G, features and dH.
 
-// The classes of a block of G are dealt to slabs for dH, so that every compute unit has a workgroup; how many are needed
-// depends on the rows with a label that there are (12839 x 352 -> 29071 bf16, a twentieth labelled, 681 -> 318 us while dH was one product).  There is room
-// for the sums of `planned` slabs of all rows; 0: the product writes dH itself, in one.
+// The classes of a block of G are dealt to slabs for dH, so that every compute unit has a workgroup; how many are
+// needed depends on the rows with a label that there are (12839 x 352 -> 29071 bf16, a twentieth labelled, 681 -> 318
+// us while dH was one product).  There is room for the sums of `planned` slabs of all rows; 0: the product writes dH
+// itself, in one.
 struct RowSlabs {
     int tiles;         // of features
     int tile_rows;
@@ -1511,12 +1516,12 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.kp = (int)(4 * up(k, 64) <= 3 * up(k, 128) ? up(k, 64) : up(k, 128));
     l.cp = (int)up(c, kTile);
     // G, four bytes a logit, is handed on in blocks of at most 2^26 logits, of 8192 classes and as many rows (us of
-    // 16384 x 512 -> 50001 bf16 and 72640 x 32 -> 8123 fp32, 2^24, 2^25, 2^26, 2^27: 8090 7080 6780 7400, 2270 1790 1610
-    // 1740; of 30000 x 200 -> 20000 bf16 with 4096 rows of 16384 classes 3490, 8192 of 8192 3150).  Where twice the rows
-    // are all of them they are one block (in two blocks 16384 x 256 -> 50001 fp32 5440 -> 5550 us, 9000 x 64 -> 60000 bf16 1510 -> 1670;
-    // 100000 x 64 -> 1000 fp32 would gain, 444 -> 394); of many features, whose sums of dH each block of classes reads and writes,
-    // where 5/4 of them are (in two blocks 16384 x 512 -> 50001 bf16 7350 -> 6920, 12000 x 384 -> 20001 fp32 2670 -> 2580, but 9000 x 512 ->
-    // 20001 bf16 1690 -> 1770).
+    // 16384 x 512 -> 50001 bf16 and 72640 x 32 -> 8123 fp32, 2^24, 2^25, 2^26, 2^27: 8090 7080 6780 7400, 2270 1790
+    // 1610 1740; of 30000 x 200 -> 20000 bf16 with 4096 rows of 16384 classes 3490, 8192 of 8192 3150).  Where twice
+    // the rows are all of them they are one block (in two blocks 16384 x 256 -> 50001 fp32 5440 -> 5550 us, 9000 x 64
+    // -> 60000 bf16 1510 -> 1670; 100000 x 64 -> 1000 fp32 would gain, 444 -> 394); of many features, whose sums of
+    // dH each block of classes reads and writes, where 5/4 of them are (in two blocks 16384 x 512 -> 50001 bf16 7350
+    // -> 6920, 12000 x 384 -> 20001 fp32 2670 -> 2580, but 9000 x 512 -> 20001 bf16 1690 -> 1770).
     const int64_t most = (int64_t)1 << 26, all_rows = up(n > 0 ? n : 1, kMostTileRows);
     int64_t cols = between(kTile, l.cp, 8192);
     // (2^18 rows at most, and 2^32 cells of dH: a launch has less than 2^32 threads)
@@ -1548,8 +1553,9 @@ Layout plan(int dtype, int64_t n, int32_t k, int32_t c, bool gradients)
     l.row_slabs = {l.kp / l.r_width, kGradRows, (int)cols, l.rows_direct ? 0 : planned, (int)rows};
     l.w_direct = l.w_slabs == 1 && l.row_pieces == 1;
     l.loss_rows = l.one_tile ? 64 : rows <= 4096 ? 4 : 16;
-    // (few rows: more lanes to each.  us with 4 and 16 rows to a block: 100 x 64 -> 60000 fp32 41 46, 96 x 256 -> 32000 bf16 with gradients 86 88,
-    // 1000 x 64 -> 5000 27 26, 4096 x 64 -> 5000 40 34; 6000 x 64 -> 5000 47 42, 10007 x 256 -> 5003 bf16 81 76)
+    // (few rows: more lanes to each.  us with 4 and 16 rows to a block: 100 x 64 -> 60000 fp32 41 46, 96 x 256 ->
+    // 32000 bf16 with gradients 86 88, 1000 x 64 -> 5000 27 26, 4096 x 64 -> 5000 40 34; 6000 x 64 -> 5000 47 42,
+    // 10007 x 256 -> 5003 bf16 81 76)
     l.list_step = (int)between(kListStep, up(ceil_div(n, 2048), kListStep), (int64_t)1 << 30);
     l.list_blocks = (int)(n > 0 ? ceil_div(n, l.list_step) : 1);
     size_t at = 0;
@@ -1627,8 +1633,9 @@ int launch_linear_xent(int dtype, const void* H, int64_t ldh, const float* W, in
     tp.list_step = l.list_step;
     tp.w_pieces = (int)ceil_div(c, kTopCols);
     tp.w_blocks = tp.w_pieces * k;
-    // (the blocks' atomics meet in a few lines: 262144 x 128 -> 172 fp32, a tenth labelled, over one input again and again, 97 us with 1024
-    // blocks, 94 with 512, 101 with 256; with 1024, 2048 or 4096 blocks to clear 105, 104, 104)
+    // (the blocks' atomics meet in a few lines: 262144 x 128 -> 172 fp32, a tenth labelled, over one input again and
+    // again, 97 us with 1024 blocks, 94 with 512, 101 with 256; with 1024, 2048 or 4096 blocks to clear 105, 104,
+    // 104)
     tp.h_rows = (int)between(64, ceil_div(n, 512), (int64_t)1 << 30);
     tp.h_blocks = (int)between(1, ceil_div(n, tp.h_rows), 512);
     tp.clear_blocks = row_loss || dH ? (int)between(0, ceil_div(n * (dH ? (k + 7) / 8 : 1), 4 * kBlock), 2048) : 0;
